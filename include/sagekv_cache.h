@@ -111,6 +111,24 @@ sagekv_status sagekvc_write(const sagekvc_desc* desc, const sagekv_paged_kv* pag
                             const int32_t* token_offsets, const int32_t* seq_lens, const int32_t* positions, void* q_out, void* K, void* V,
                             void* hip_stream);
 
+/* Attention of one new token per problem over the full cache:
+ *     out[p][h] = sum_t softmax_t( q[p][h] . K[p][c][t] / sqrt(head_dim) ) V[p][c][t],   c = h / G,   t in [0, len_p),
+ * len_p = seq_lens[p] kept within [0, max_len], and, where n_recent > 0, only the tokens t < n_sink and t >= len_p - n_recent (sink and recent
+ * window over a cache from which nothing has been evicted).  n_recent = 0 (and n_sink = 0): every token.
+ *   q         [n_problems, n_q_heads, head_dim] contiguous;
+ *   seq_lens  device int32 [n_problems], read by the launch: one recorded graph serves growing sequences;
+ *   max_len   the longest length any problem may have at the launch, 1 <= max_len <= capacity;
+ *   out       [n_problems, n_q_heads, head_dim] fp32, contiguous;
+ *   lse       nullable, [n_problems, n_q_heads] fp32: log of the sum of exp(logits), with which two parts of a row can be joined.
+ * A problem that attends nothing (length 0) gets out = 0 and lse = -infinity.  What the cache holds in places that are not attended (pages' ends, an
+ * evicted middle) does not matter, whatever it is; table entries are kept within [0, n_pages), pages may be shared.  Products are exact, softmax weights and
+ * sums fp32 with a bf16 cache; logits and sums fp64 with an fp32 one.
+ * workspace: sagekvc_attn_workspace_bytes(desc), any contents; two calls that may run at the same time need one each. */
+size_t sagekvc_attn_workspace_bytes(const sagekvc_desc* desc);
+sagekv_status sagekvc_attn(const sagekvc_desc* desc, const sagekv_paged_kv* pages /* NULL: dense */, const void* q, const void* K, const void* V,
+                           const int32_t* seq_lens, int32_t max_len, int32_t n_sink, int32_t n_recent, float* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

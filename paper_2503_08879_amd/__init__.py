@@ -15,5 +15,6 @@ from .binding import (  # noqa: F401
 )
 from .full_cache import (  # noqa: F401
     ROTARY_HALF, ROTARY_PAIRS, SCALING_LINEAR, SCALING_NONE, SCALING_PARTS, SCALING_YARN, CacheDesc, NewTokens, RotaryDesc, RotaryMap, RotaryScaling,
-    cache_desc, new_tokens, paged_cache_desc, rotary, rotary_desc, sagekvc_rotary, sagekvc_rotary_frequencies, sagekvc_write,
+    cache_desc, new_tokens, paged_cache_desc, rotary, rotary_desc, sagekvc_attn, sagekvc_attn_workspace_bytes, sagekvc_rotary,
+    sagekvc_rotary_frequencies, sagekvc_write,
 )

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsagekv.so")
-SOURCES = ["api.hip", "score.hip", "select.hip", "prefilter.hip", "decode.hip", "cache_api.hip", "rotary.hip"]
+SOURCES = ["api.hip", "score.hip", "select.hip", "prefilter.hip", "decode.hip", "cache_api.hip", "cache_attn.hip", "rotary.hip"]
 HEADERS = ["device_utils.h", "kernels.h", "radix_select.h", os.path.join("..", "..", "include", "sagekv.h"),
            os.path.join("..", "..", "include", "sagekv_bench.h"), "full_cache.h", os.path.join("..", "..", "include", "sagekv_cache.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",

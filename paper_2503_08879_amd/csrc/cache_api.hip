@@ -116,6 +116,20 @@ sagekv_status check_cache(const sagekvc_desc* d, const sagekv_paged_kv* pg, cons
   return SAGEKV_OK;
 }
 
+struct AttnLayout {
+  size_t acc, ml, joins, total;
+};
+// Scratch for kAttnGroups workgroups, however many a call has: sizes are part of the interface.
+AttnLayout attn_layout(const sagekvc_desc* d) {
+  const size_t heads = (size_t)2 * kAttnGroups * (d->n_q_heads / d->n_kv_heads);
+  AttnLayout l;
+  l.acc = 0;
+  l.ml = heads * d->head_dim * sizeof(float);
+  l.joins = l.ml + heads * sizeof(float2);
+  l.total = l.joins + kAttnGroups * sizeof(JoinRecord);
+  return l;
+}
+
 }  // namespace
 
 extern "C" {
@@ -216,6 +230,60 @@ sagekv_status sagekvc_write(const sagekvc_desc* d, const sagekv_paged_kv* pages,
   p.positions = positions;
   set_map(m, &p);
   return dev(launch_rotary(p, (hipStream_t)hip_stream));
+}
+
+size_t sagekvc_attn_workspace_bytes(const sagekvc_desc* d) {
+  FullCache c;
+  // (the strides of a paged cache's problems are not looked at, and the caches' addresses neither)
+  sagekvc_desc one = d ? *d : sagekvc_desc{};
+  one.k_stride_problem = one.k_stride_head = one.v_stride_problem = one.v_stride_head = 0;
+  one.k_stride_token = one.v_stride_token = one.head_dim;
+  const void* any = (const void*)16;
+  if (check_cache(d ? &one : nullptr, nullptr, any, any, false, &c) != SAGEKV_OK) return 0;
+  return attn_layout(d).total;
+}
+
+sagekv_status sagekvc_attn(const sagekvc_desc* d, const sagekv_paged_kv* pages, const void* q, const void* K, const void* V,
+                           const int32_t* seq_lens, int32_t max_len, int32_t n_sink, int32_t n_recent, float* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+  CacheAttnParams p = {};
+  sagekv_status st = check_cache(d, pages, K, V, false, &p.cache);
+  if (st != SAGEKV_OK) return st;
+  if (!q || !seq_lens || !out || max_len < 1 || max_len > d->capacity || n_sink < 0 || n_recent < 0 || (n_recent == 0 && n_sink > 0))
+    return SAGEKV_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(seq_lens, 4) || !aligned(out, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return SAGEKV_ERR_UNSUPPORTED;
+  const AttnLayout l = attn_layout(d);
+  if (!workspace || workspace_bytes < l.total) return SAGEKV_ERR_WORKSPACE;
+  p.q = (const char*)q;
+  p.out = out;
+  p.lse = lse;
+  p.lens = seq_lens;
+  p.P = d->n_problems;
+  p.Hq = d->n_q_heads;
+  p.Hkv = d->n_kv_heads;
+  p.G = d->n_q_heads / d->n_kv_heads;
+  p.D = d->head_dim;
+  p.dtype = d->dtype;
+  p.S = n_sink < max_len ? n_sink : max_len;
+  p.W = n_recent < max_len ? n_recent : max_len;
+  p.max_len = max_len;
+  p.scale = (float)(1.0 / sqrt((double)d->head_dim));
+  p.join_scale = d->dtype == SAGEKV_BF16 ? p.scale : 1.f;
+  // steps of the longest row: all of its tokens, or those of the window's two ends
+  int64_t steps = ((int64_t)max_len + kStep - 1) / kStep;
+  if (p.W > 0) {
+    const int64_t ends = (p.S + kStep - 1) / kStep + (p.W + kStep - 2) / kStep + 1;
+    if (ends < steps) steps = ends;
+  }
+  // up to two steps a row is one unit, and there is nothing to join
+  p.per_unit = steps <= 2 ? (int)steps : 1;
+  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads, units = rows * ((steps + p.per_unit - 1) / p.per_unit);
+  if (units > 0x7FFFFFFF) return SAGEKV_ERR_UNSUPPORTED;
+  p.n_groups = units < kAttnGroups ? (int)units : kAttnGroups;
+  p.part_acc = (float*)((char*)workspace + l.acc);
+  p.part_ml = (float2*)((char*)workspace + l.ml);
+  p.joins = (JoinRecord*)((char*)workspace + l.joins);
+  return dev(launch_cache_attn(p, steps > p.per_unit, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

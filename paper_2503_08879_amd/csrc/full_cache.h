@@ -33,4 +33,30 @@ struct RotaryParams {
 };
 hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
 
+constexpr int kStep = 128;      // tokens the four waves of an attention workgroup take at a time
+constexpr int kAttnGroups = 512;  // workgroups of an attention launch at most
+
+// Where a workgroup's first row, if it began in an earlier workgroup, is to be joined: see cache_attn.hip.
+struct JoinRecord {
+  int row, first, last, first_slot;  // first < 0: nothing to do
+};
+
+struct CacheAttnParams {
+  FullCache cache;
+  const char* q;
+  float *out, *lse;
+  const int32_t* lens;
+  int P, Hq, Hkv, G, D, dtype;
+  int S, W, max_len;
+  int per_unit;  // steps of a unit of work; a unit is never split
+  int n_groups;  // workgroups
+  int g0, gb;    // the group's heads that a launch handles
+  float scale;       // 1 / sqrt(head_dim)
+  float join_scale;  // the parts' maxima times this are logits: scale where they are products (bf16), 1 where they are logits (fp32)
+  float* part_acc;    // [n_groups][2][G][D]
+  float2* part_ml;    // [n_groups][2][G]
+  JoinRecord* joins;  // [n_groups]
+};
+hipError_t launch_cache_attn(const CacheAttnParams& p, bool join, hipStream_t s);
+
 }  // namespace sagekv

@@ -15,7 +15,7 @@ from .binding import PagedKV, _check, _dtype_of, _stream, lib
 ROTARY_HALF, ROTARY_PAIRS = 0, 1
 SCALING_NONE, SCALING_LINEAR, SCALING_PARTS, SCALING_YARN = 0, 1, 2, 3
 
-EXPORTS = ("sagekvc_rotary_frequencies", "sagekvc_rotary", "sagekvc_write")
+EXPORTS = ("sagekvc_rotary_frequencies", "sagekvc_rotary", "sagekvc_write", "sagekvc_attn_workspace_bytes", "sagekvc_attn")
 
 _i32, _i64, _vp = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 
@@ -48,11 +48,13 @@ class NewTokens(ctypes.Structure):
 @functools.lru_cache(maxsize=None)
 def _fn(name):
     f = getattr(lib(), name)
-    f.restype = ctypes.c_int
+    f.restype = ctypes.c_size_t if name.endswith("_bytes") else ctypes.c_int
     f.argtypes = {
         "sagekvc_rotary_frequencies": [_i32, ctypes.c_double, _vp, _vp, _vp],
         "sagekvc_rotary": [_vp] * 6,
         "sagekvc_write": [_vp] * 14,
+        "sagekvc_attn_workspace_bytes": [_vp],
+        "sagekvc_attn": [_vp] * 6 + [_i32] * 3 + [_vp] * 3 + [ctypes.c_size_t, _vp],
     }[name]
     return f
 
@@ -206,3 +208,29 @@ def sagekvc_write(desc: CacheDesc, pages, tokens: NewTokens, rot, q, k_new, v_ne
 def _heads(t, n):
     if t is not None and t.shape[1] != n:
         raise ValueError(f"{n} heads are expected, got {t.shape[1]}")
+
+
+def sagekvc_attn_workspace_bytes(desc: CacheDesc) -> int:
+    return _fn("sagekvc_attn_workspace_bytes")(ctypes.byref(desc))
+
+
+def _floats(t, n):
+    """Address of a float32 tensor of n elements without gaps on the current GPU; None stays None."""
+    if t is None:
+        return None
+    if _at(t, binding.F32) and (t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"expected {n} contiguous float32 values, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def sagekvc_attn(desc: CacheDesc, pages, q, K, V, seq_lens, max_len: int, n_sink: int, n_recent: int, out, lse, workspace) -> None:
+    """Attention of one new token per problem, q [P, Hq, d], over the first seq_lens[p] (int32 [P], at most max_len) tokens of the full cache; n_recent > 0:
+    over the first n_sink and the last n_recent of them.  out float32 [P, Hq, d]; lse float32 [P, Hq] or None."""
+    heads = desc.n_problems * desc.n_q_heads
+    if q.numel() != heads * desc.head_dim or not q.is_contiguous():
+        raise ValueError("q: [problems, heads, head_dim], contiguous, is expected")
+    if not workspace.is_cuda or workspace.get_device() != _current_device():
+        raise ValueError("workspace: memory of the current GPU is expected")
+    _check(_fn("sagekvc_attn")(ctypes.byref(desc), _ref(pages), _at(q, desc.dtype), _at(K, desc.dtype), _at(V, desc.dtype),
+                               _ints(seq_lens, desc.n_problems), max_len, n_sink, n_recent, _floats(out, heads * desc.head_dim), _floats(lse, heads),
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "sagekvc_attn")

@@ -187,6 +187,40 @@ def test_write_without_descriptors_and_of_no_tokens():
     assert f(byref(desc), byref(pages), byref(tokens), byref(rot), None, None, None, P16, P16, None, None, P16, P16, None) == OK
 
 
+@pytest.mark.parametrize("code,paged,change", CACHE_REFUSALS + [
+    (INVALID, True, dict(q=None)), (UNSUPPORTED, True, dict(q=P16 + 8)), (INVALID, True, dict(out=None)), (UNSUPPORTED, True, dict(out=P16 + 2)),
+    (UNSUPPORTED, True, dict(lse=P16 + 1)), (INVALID, True, dict(max_len=0)), (INVALID, True, dict(max_len=101)), (INVALID, True, dict(S=-1)),
+    (INVALID, True, dict(W=-1)), (INVALID, True, dict(S=4, W=0)), (WORKSPACE, True, dict(ws=None)), (WORKSPACE, True, dict(short=1)),
+    (UNSUPPORTED, True, dict(ws=P16 + 8)),
+])
+def test_attn_refusals(code, paged, change):
+    own = dict(out=P16, lse=P16, ws=P16, max_len=100, S=0, W=0, short=0)
+    own.update({k: v for k, v in change.items() if k in own})
+    size = sk.sagekvc_attn_workspace_bytes(cache_args(paged)[0])
+    assert size > 0
+    desc, pages, _, _, a = cache_args(paged, **{k: v for k, v in change.items() if k not in own})
+    got = fc._fn("sagekvc_attn")(byref(desc), fc._ref(pages), a["q"], a["K"], a["V"], a["lens"], own["max_len"], own["S"], own["W"], own["out"], own["lse"],
+                                 own["ws"], size - own["short"], None)
+    assert got == code
+
+
+def test_attn_of_more_work_than_can_be_numbered():
+    """65535 rows of 2^31 tokens, all through strides of 0: more than 2^31 steps."""
+    desc = sk.CacheDesc(65535, 1, 1, 64, sk.BF16, 0x7FFFFFF0, 0, 0, 64, 0, 0, 64)
+    f = fc._fn("sagekvc_attn")
+    size = sk.sagekvc_attn_workspace_bytes(desc)
+    assert f(byref(desc), None, P16, P16, P16, P16, 0x7FFFFFF0, 0, 0, P16, None, P16, size, None) == UNSUPPORTED
+
+
+def test_attn_workspace():
+    n = fc._fn("sagekvc_attn_workspace_bytes")
+    assert n(None) == 0
+    desc = sk.CacheDesc(3, 8, 2, 128, sk.BF16, 100, 0, 0, 0, 0, 0, 0)  # strides do not enter
+    assert n(byref(desc)) == 2 * 512 * 4 * (128 * 4 + 8) + 512 * 16
+    desc.head_dim = 96
+    assert n(byref(desc)) == 0
+
+
 def test_descriptor_makers_refuse_tensors_they_cannot_describe():
     import torch
 

@@ -1,0 +1,342 @@
+"""Attention of one new token per problem over the full cache on the GPU, against fp64."""
+import numpy as np
+import pytest
+
+from tests import cache_util as cu
+from tests.test_gpu_rotary import gen
+
+pytestmark = pytest.mark.gpu
+STEP = 2.0 ** -24
+
+
+def bound(q, K, V, S, W, f32):
+    """Error an output element and the log-sum-exp of each head may have.  A weight's relative error: its logit's absolute error plus a few steps of
+    2^-24 for the exponential.  bf16: a logit's 128 exact products are added in fp32, off by 16 steps of scale * sum |q k| (roundings of either sign; all of one
+    sign would be 128), and the difference to the maximum is rounded; fp32 caches form both in fp64 and round the difference.  The sum over the tokens is
+    rounded once per 32 tokens and wave, and in the joins: 64 + tokens / 128 steps of sum p |v|."""
+    Hq, d = q.shape
+    G = Hq // K.shape[0]
+    n = K.shape[1]
+    t = np.arange(n)
+    if W:
+        t = t[(t < S) | (t >= n - W)]
+    out, lse = np.zeros((Hq, d)), np.zeros(Hq)
+    if not len(t):
+        return out, lse
+    for h in range(Hq):
+        k, v = K[h // G][t], V[h // G][t]
+        x = k @ q[h] / np.sqrt(d)
+        w = np.exp(x - x.max())
+        w /= w.sum()
+        size = 0.0 if f32 else 16 * (np.abs(k) @ np.abs(q[h])).max() / np.sqrt(d)
+        e = STEP * (size + 64 + len(t) / 128) + STEP * 4 * (w * (x.max() - x)).sum()
+        out[h] = e * (w @ np.abs(v)) * 2  # numerator and denominator
+        lse[h] = e + STEP * 4 * abs(x.max() + 1)
+    return out, lse
+
+
+def case(lens, Hq, Hkv, d, dtype="bfloat16", dense=False, order="heads", page=16, S=0, W=0, cap=None, max_len=None, q_scale=1.0, seed=0, poison=True,
+         stream=None, lse=True, edit=None, check=None):
+    """Runs one call over problems of the given lengths; what lies behind them, or in front of the window, is NaN."""
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    g, t, P = gen(seed + sum(lens) + d), getattr(torch, dtype), len(lens)
+    cap = max(max(lens), 1) if cap is None else cap
+    q = (torch.randn((P, Hq, d), generator=g, device="cuda") * q_scale).to(t)
+    if dense:
+        K, V = (torch.randn((P, Hkv, cap, d) if order == "heads" else (P, cap, Hkv, d), generator=g, device="cuda").to(t) for _ in range(2))
+        if order == "tokens":
+            K, V = K.transpose(1, 2), V.transpose(1, 2)
+        Kd, Vd = cu.f64(K), cu.f64(V)
+        desc, pages, table = sk.cache_desc(K, V, Hq), None, None
+    else:
+        pg = cu.Pages(g, P, Hkv, d, cap, page, t, order)
+        K, V, table = pg.K, pg.V, pg.table
+        Kd, Vd = pg.dense(K), pg.dense(V)
+    if poison:
+        for x in (K, V):
+            for p, n in enumerate(lens):
+                dead = torch.ones(x.shape[2] if dense else pg.per * page, dtype=torch.bool, device="cuda")
+                dead[:n] = False
+                if W and n > S + W:
+                    dead[S:n - W] = True
+                if dense:
+                    x[p][:, dead] = float("nan")
+                else:
+                    at = dead.nonzero().reshape(-1)
+                    x[table[p, at // page].long(), :, at % page] = float("nan")
+    if not dense:
+        if edit:
+            edit(table, K.shape[0])
+        desc, pages = sk.paged_cache_desc(K, V, table, Hq, cap)
+    seq = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out = torch.full((P, Hq, d), float("nan"), device="cuda")
+    ls = torch.full((P, Hq), float("nan"), device="cuda") if lse else None
+    ws = torch.randint(0, 256, (sk.sagekvc_attn_workspace_bytes(desc),), generator=g, device="cuda", dtype=torch.uint8)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream or torch.cuda.current_stream()):
+        sk.sagekvc_attn(desc, pages, q, K, V, seq, cap if max_len is None else max_len, S, W, out, ls, ws)
+    torch.cuda.synchronize()
+    got, got_l, q64 = cu.f64(out), None if ls is None else cu.f64(ls), cu.f64(q)
+    worst = 0.0
+    for p, n in enumerate(lens):
+        if check is not None and p not in check:
+            continue
+        n = max(0, min(n, cap if max_len is None else max_len))
+        args = (q64[p], Kd[p][:, :n], Vd[p][:, :n], S, W)
+        want, want_l = cu.attention(*args)
+        b, bl = bound(*args, dtype == "float32")
+        assert np.isfinite(got[p]).all(), p
+        err = np.abs(got[p] - want)
+        worst = max(worst, (err / np.maximum(b, 1e-300)).max() if n else err.max())
+        assert (err <= b).all(), f"problem {p} of {n} tokens: {(err / np.maximum(b, 1e-300)).max():.3g} times the bound"
+        if ls is not None:
+            if n == 0:
+                assert (got_l[p] == -np.inf).all()
+            else:
+                assert (np.abs(got_l[p] - want_l) <= bl).all(), p
+    return worst
+
+
+EDGES = [0, 1, 15, 16, 17, 31, 32, 33, 0, 127, 128, 129, 255, 256, 257, 300, 1000, 2049]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("dense,order,page", [(True, "heads", 16), (True, "tokens", 16), (False, "heads", 16), (False, "tokens", 32), (False, "heads", 256)])
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 128), (7, 1, 64), (3, 3, 128), (4, 2, 64), (32, 2, 128)])
+def test_ragged_lengths(dtype, dense, order, page, Hq, Hkv, d):
+    case(EDGES, Hq, Hkv, d, dtype, dense, order, page)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 6, 7, 8, 9, 12, 16, 17, 24, 33, 64])
+def test_heads_per_group(dtype, d, G):
+    case([600, 3, 0, 130], 2 * G, 2, d, dtype, seed=G)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("n", [1, 2, 16, 128, 129, 256, 257, 384, 640, 5000, 70001])
+def test_one_sequence(dtype, n):
+    """Rows from one token to many steps, alone and with a capacity beyond them."""
+    case([n], 8, 2, 128, dtype, seed=n)
+    case([n], 4, 4, 64, dtype, dense=True, cap=n + 700, seed=n)
+
+
+@pytest.mark.parametrize("P", [2, 63, 64, 65, 128, 513, 4097])
+def test_many_problems(P):
+    """The share of every workgroup is found from lengths of 64 problems at a time, of 64 * 64, ..."""
+    rng = np.random.default_rng(P)
+    lens = [int(x) for x in rng.integers(0, 40, P)]
+    for p in rng.integers(0, P, 4):
+        lens[p] = int(rng.integers(200, 700))
+    check = set(range(P)) if P < 600 else set(int(x) for x in rng.integers(0, P, 300)) | {0, P - 1} | {p for p in range(P) if lens[p] > 100}
+    case(lens, 4, 2, 64, check=check)
+    case([0] * (P - 1) + [500], 4, 2, 64, check={0, P - 2, P - 1})
+    case([500] + [0] * (P - 1), 4, 2, 64, "float32", dense=True, check={0, 1, P - 1})
+
+
+def test_nothing_to_attend_anywhere():
+    case([0, 0, 0], 4, 2, 128, cap=300)
+    case([0], 4, 2, 64, "float32", dense=True, cap=1)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("S,W", [(0, 1), (4, 1), (0, 128), (4, 60), (130, 200), (128, 128), (1, 1000), (200, 1), (3, 5000), (1000, 1000)])
+@pytest.mark.parametrize("dense", [True, False])
+def test_sink_and_recent_window(dtype, S, W, dense):
+    lens = [0, 1, 5, 64, 65, 129, 200, 256, 330, 331, 500, 1001, 1400, 3001]
+    case(lens, 8, 2, 64 if dense else 128, dtype, dense, S=S, W=W, page=32)
+
+
+def test_lengths_beyond_the_longest_are_cut_there():
+    case([100, 700, 512, 513], 4, 2, 128, cap=700, max_len=512)
+    case([-5, 0, 3], 4, 2, 128, cap=700, max_len=3)
+
+
+def test_page_entries_behind_a_row_do_not_matter_and_bad_ones_are_kept_inside():
+    def behind(table, n):
+        table[0, 7:], table[1, 2:], table[2, :] = -1, 2 ** 31 - 1, -7
+
+    case([112, 30, 0], 4, 2, 128, cap=300, edit=behind)
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    g = gen(4)
+    K, V = (torch.randn((3, 1, 16, 64), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((2, 1, 64), generator=g, device="cuda").bfloat16()
+    table = torch.tensor([[-1, 1], [99, 1]], dtype=torch.int32, device="cuda")  # the first page, the last one
+    desc, pages = sk.paged_cache_desc(K, V, table, 1)
+    out, ws = torch.empty((2, 1, 64), device="cuda"), torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    sk.sagekvc_attn(desc, pages, q, K, V, torch.tensor([20, 20], dtype=torch.int32, device="cuda"), 32, 0, 0, out, None, ws)
+    for p, first in ((0, 0), (1, 2)):
+        k, v = (torch.cat([x[first, 0], x[1, 0, :4]])[None] for x in (K, V))
+        want, _ = cu.attention(cu.f64(q[p]), cu.f64(k), cu.f64(v))
+        assert np.abs(cu.f64(out[p]) - want).max() < 1e-5  # values of size 1, fp32 sums
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("q_scale", [0.0, 8.0, 40.0])
+def test_flat_and_peaked_weights(dtype, q_scale):
+    case([900, 1, 300, 64], 8, 2, 128, dtype, q_scale=q_scale)
+    case([900, 1, 300, 64], 14, 2, 64, dtype, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("G", [1, 3, 6, 12])
+def test_infinite_values_and_keys_that_are_attended(dtype, G):
+    """An infinite value makes its own dim infinite, nothing else; a key that makes the logit -infinity has no weight; NaN stays with its row."""
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    g, t, d, n = gen(G), getattr(torch, dtype), 128, 400
+    K, V = (torch.randn((3, 1, n, d), generator=g, device="cuda").to(t) for _ in range(2))
+    q = torch.rand((3, G, d), generator=g, device="cuda").add_(0.5).to(t)
+    K[0, 0, 399] = float("-inf")   # q > 0: logit -infinity
+    K[0, 0, 7] = q[0].float().mean(0).to(t)  # a weight that is 1 or nearly, so that some of its parts are 0
+    V[0, 0, 7, 5], V[0, 0, 200, 90] = float("inf"), float("-inf")
+    V[1, 0, 3, 17] = float("nan")
+    desc = sk.cache_desc(K, V, G)
+    out, lse = torch.zeros((3, G, d), device="cuda"), torch.zeros((3, G), device="cuda")
+    ws = torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    sk.sagekvc_attn(desc, None, q, K, V, torch.tensor([n, n, n], dtype=torch.int32, device="cuda"), n, 0, 0, out, lse, ws)
+    assert (out[0, :, 5] == float("inf")).all() and (out[0, :, 90] == float("-inf")).all()
+    fine = torch.ones(d, dtype=torch.bool)
+    fine[[5, 90]] = False
+    k, v = cu.f64(K[0]), np.where(np.isfinite(cu.f64(V[0])), cu.f64(V[0]), 0.0)
+    want, want_l = cu.attention(cu.f64(q[0]), np.delete(k, 399, 1), np.delete(v, 399, 1))
+    b, _ = bound(cu.f64(q[0]), np.delete(k, 399, 1), np.delete(v, 399, 1), 0, 0, dtype == "float32")
+    assert (np.abs(cu.f64(out[0]) - want) <= b)[:, fine.numpy()].all()
+    assert torch.isnan(out[1, :, 17]).all() and torch.isfinite(out[1][:, [i for i in range(d) if i != 17]]).all()
+    assert torch.isfinite(out[2]).all() and torch.isfinite(lse).all()
+
+
+def test_every_key_impossible():
+    """All logits -infinity: nothing is attended."""
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    for t in (torch.bfloat16, torch.float32):
+        K = torch.full((1, 1, 300, 64), float("-inf"), device="cuda", dtype=t)
+        V = torch.ones_like(K)
+        q = torch.ones((1, 2, 64), device="cuda", dtype=t)
+        desc = sk.cache_desc(K, V, 2)
+        out, lse = torch.ones((1, 2, 64), device="cuda"), torch.ones((1, 2), device="cuda")
+        ws = torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+        sk.sagekvc_attn(desc, None, q, K, V, torch.tensor([300], dtype=torch.int32, device="cuda"), 300, 0, 0, out, lse, ws)
+        assert not out.any() and (lse == float("-inf")).all()
+
+
+def test_shared_pages_broadcast_caches_and_no_lse():
+    """Several problems may read the same pages; so may all through a stride of 0."""
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    g = gen(30)
+    K, V = (torch.randn((1, 2, 500, 64), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((5, 4, 64), generator=g, device="cuda").bfloat16()
+    Ke, Ve = K.expand(5, 2, 500, 64), V.expand(5, 2, 500, 64)
+    desc = sk.cache_desc(Ke, Ve, 4)
+    out, ws = torch.empty((5, 4, 64), device="cuda"), torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    lens = [500, 1, 77, 0, 300]
+    sk.sagekvc_attn(desc, None, q, Ke, Ve, torch.tensor(lens, dtype=torch.int32, device="cuda"), 500, 0, 0, out, None, ws)
+    for p, n in enumerate(lens):
+        args = (cu.f64(q[p]), cu.f64(K[0, :, :n]), cu.f64(V[0, :, :n]))
+        assert (np.abs(cu.f64(out[p]) - cu.attention(*args)[0]) <= bound(*args, 0, 0, False)[0]).all()
+
+
+def test_two_parts_joined_by_their_log_sums():
+    """The purpose of lse: the halves of a row, attended apart, joined, are the row."""
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    g = gen(31)
+    K, V = (torch.randn((1, 2, 700, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((1, 8, 128), generator=g, device="cuda").bfloat16()
+    res = []
+    for a, b in ((0, 450), (450, 700), (0, 700)):
+        k, v = K[:, :, a:b], V[:, :, a:b]
+        desc = sk.cache_desc(k, v, 8)
+        out, lse = torch.empty((1, 8, 128), device="cuda"), torch.empty((1, 8), device="cuda")
+        ws = torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+        sk.sagekvc_attn(desc, None, q, k, v, torch.tensor([b - a], dtype=torch.int32, device="cuda"), b - a, 0, 0, out, lse, ws)
+        res.append((cu.f64(out), cu.f64(lse)[..., None]))
+    (o1, l1), (o2, l2), (o, l) = res
+    t = np.logaddexp(l1, l2)
+    assert np.abs(o1 * np.exp(l1 - t) + o2 * np.exp(l2 - t) - o).max() < 2e-6 and np.abs(t - l).max() < 2e-6
+
+
+def test_cache_beyond_32_bits():
+    """Pages and dense rows further than 2^31 elements and 2^32 bytes from the pool's start."""
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    n = (1 << 20) + 40  # pages of 16 x 128 bf16: 4 KB each
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("not enough memory")
+    g = gen(6)
+    K = torch.zeros((n, 1, 16, 128), device="cuda", dtype=torch.bfloat16)
+    V = torch.zeros_like(K)
+    far = [n - 1, n - 30, 5, n - 7, n // 2 + 3]
+    K[far], V[far] = (torch.randn((5, 1, 16, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((1, 4, 128), generator=g, device="cuda").bfloat16()
+    desc, pages = sk.paged_cache_desc(K, V, torch.tensor([far], dtype=torch.int32, device="cuda"), 4)
+    out, ws = torch.empty((1, 4, 128), device="cuda"), torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    sk.sagekvc_attn(desc, pages, q, K, V, torch.tensor([75], dtype=torch.int32, device="cuda"), 80, 0, 0, out, None, ws)
+    args = (cu.f64(q[0]), cu.f64(K[far, 0].reshape(1, 80, 128)[:, :75]), cu.f64(V[far, 0].reshape(1, 80, 128)[:, :75]))
+    assert (np.abs(cu.f64(out[0]) - cu.attention(*args)[0]) <= bound(*args, 0, 0, False)[0]).all()
+    # a dense row of 2^23 tokens, the second problem's far end: only the last 100 tokens have weight
+    Kd, Vd = (x.view(2, 1, -1, 128) for x in (K, V))
+    rows = Kd.shape[2]
+    Kd[1, 0, :] = -q[0].float().mean(0).bfloat16() * 40
+    Kd[1, 0, -100:], Vd[1, 0, -100:] = (torch.randn((100, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q2 = q[:, :1].expand(2, 1, 128).contiguous()
+    desc = sk.cache_desc(Kd, Vd, 1)
+    out, ws = torch.empty((2, 1, 128), device="cuda"), torch.empty(sk.sagekvc_attn_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    sk.sagekvc_attn(desc, None, q2, Kd, Vd, torch.tensor([1, rows], dtype=torch.int32, device="cuda"), rows, 0, 100, out, None, ws)
+    args = (cu.f64(q2[1]), cu.f64(Kd[1, :, -100:]), cu.f64(Vd[1, :, -100:]))
+    assert (np.abs(cu.f64(out[1]) - cu.attention(*args)[0]) <= bound(*args, 0, 0, False)[0]).all()
+
+
+def test_streams_at_once_and_a_replayed_graph_of_growing_sequences():
+    import torch
+
+    import paper_2503_08879_amd as sk
+
+    g = gen(12)
+    P, Hq, Hkv, d, cap = 6, 8, 2, 128, 900
+    pg = cu.Pages(g, P, Hkv, d, cap, 16, torch.bfloat16)
+    desc, pages = sk.paged_cache_desc(pg.K, pg.V, pg.table, Hq, cap)
+    q = torch.randn((P, Hq, d), generator=g, device="cuda").bfloat16()
+    lens = torch.tensor([1, 127, 0, 640, 255, 511], dtype=torch.int32, device="cuda")
+    size = sk.sagekvc_attn_workspace_bytes(desc)
+    ws, ws2 = (torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2))
+    outs = [torch.zeros((P, Hq, d), device="cuda") for _ in range(3)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sk.sagekvc_attn(desc, pages, q, pg.K, pg.V, lens, cap, 0, 0, outs[2], None, ws)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                outs[k].zero_()
+                sk.sagekvc_attn(desc, pages, q, pg.K, pg.V, lens, cap, 0, 0, outs[k], None, (ws, ws2)[k])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sk.sagekvc_attn(desc, pages, q, pg.K, pg.V, lens, cap, 0, 0, outs[0], None, ws)
+    for _ in range(5):
+        sk.sagekvc_attn(desc, pages, q, pg.K, pg.V, lens, cap, 0, 0, outs[1], None, ws)  # on the same workspace
+        outs[0].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1])
+        lens.add_(torch.tensor([1, 1, 70, 1, 1, 130], dtype=torch.int32, device="cuda"))
