@@ -269,21 +269,23 @@ sagekv_status sagekvc_attn(const sagekvc_desc* d, const sagekv_paged_kv* pages, 
   p.max_len = max_len;
   p.scale = (float)(1.0 / sqrt((double)d->head_dim));
   p.join_scale = d->dtype == SAGEKV_BF16 ? p.scale : 1.f;
-  // steps of the longest row: all of its tokens, or those of the window's two ends
-  int64_t steps = ((int64_t)max_len + kStep - 1) / kStep;
+  // blocks of the longest row: all of its tokens, or those of the window's two ends
+  int64_t blocks = ((int64_t)max_len + kBlock - 1) / kBlock;
   if (p.W > 0) {
-    const int64_t ends = (p.S + kStep - 1) / kStep + (p.W + kStep - 2) / kStep + 1;
-    if (ends < steps) steps = ends;
+    const int64_t ends = (p.S + kBlock - 1) / kBlock + (p.W + kBlock - 2) / kBlock + 1;
+    if (ends < blocks) blocks = ends;
   }
-  // up to two steps a row is one unit, and there is nothing to join
-  p.per_unit = steps <= 2 ? (int)steps : 1;
-  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads, units = rows * ((steps + p.per_unit - 1) / p.per_unit);
-  if (units > 0x7FFFFFFF) return SAGEKV_ERR_UNSUPPORTED;
-  p.n_groups = units < kAttnGroups ? (int)units : kAttnGroups;
+  // up to two rounds of a workgroup's waves: rows are left whole, and there is nothing to join
+  p.whole_rows = blocks <= 2 * kGroupBlocks;
+  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads, weight = rows * (p.whole_rows ? 1 : blocks + kRowWeight);
+  if (weight > 0x7FFFFFFF - kGroupBlocks) return SAGEKV_ERR_UNSUPPORTED;
+  const int64_t busy = p.whole_rows ? weight : (weight + kGroupBlocks - 1) / kGroupBlocks;
+  p.n_groups = busy < kAttnGroups ? (int)busy : kAttnGroups;
+  p.by_row = rows <= kAttnGroups;
   p.part_acc = (float*)((char*)workspace + l.acc);
   p.part_ml = (float2*)((char*)workspace + l.ml);
   p.joins = (JoinRecord*)((char*)workspace + l.joins);
-  return dev(launch_cache_attn(p, steps > p.per_unit, (hipStream_t)hip_stream));
+  return dev(launch_cache_attn(p, !p.whole_rows, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

@@ -1,10 +1,10 @@
 // Attention of one new token per sequence over the full cache, every sequence of its own length.
 //
-// A row (sequence, KV head) is cut into steps of 128 tokens and the steps into units (usually one step each).  The units of all rows, one row
-// after the other, are divided evenly over the launch's workgroups, whatever the lengths: a workgroup finds its share from the
-// lengths alone, which it reads on the device (64 of them at a time, summed over the wave).  A row that one workgroup has for itself is written
-// straight to `out`; parts of a row shared by several go to scratch (a workgroup has two at most, its first row's and its last one's)
-// and join_kernel merges them, (max, sum, accumulator) by (max, sum, accumulator).
+// A row (sequence, KV head) is cut into blocks of 32 tokens.  All rows, one after the other, are divided over the launch's workgroups, whatever their
+// lengths: a row weighs its blocks and kRowWeight more for its beginning and end, and every workgroup gets the same weight.  It finds its share from the
+// lengths alone, which it reads on the device (64 of them at a time, summed over the wave).  A row that one workgroup has for itself is written straight
+// to `out`; parts of a row shared by several go to scratch, at most two a workgroup: one that continues a row and one that begins
+// one.  join_kernel merges them, (max, sum, accumulator) by (max, sum, accumulator).
 //
 // Bound by HBM: K and V are read once, for all heads of the group at a time.
 #include "device_utils.h"
@@ -14,21 +14,27 @@ namespace sagekv {
 
 namespace {
 
-// ---- lengths, steps and units ------------------------------------------------------------------
-// The steps of a row of len tokens: all that hold attended tokens.  With a window those of the first S and of the last W tokens.
-struct RowSteps {
-  int len, n;      // tokens; steps
-  int head, skip;  // steps from `head` on lie `skip` steps further
-  __device__ __forceinline__ int token(int step) const { return (step < head ? step : step + skip) * kStep; }
+// ---- rows, weights and shares ------------------------------------------------------------------
+// Lengths do not change while a launch runs: through the constant address space they come by scalar loads, which nothing else waits for.  (A vector
+// load of a length in the middle of a share waits for all of K and V that is in flight.)
+__device__ __forceinline__ int length_of(const CacheAttnParams& p, int prob) {
+  return ((const __attribute__((address_space(4))) int*)p.lens)[prob];
+}
+
+// The blocks of a row of len tokens that hold attended tokens.  With a window those of the first S and of the last W tokens.
+struct RowBlocks {
+  int len, n;      // tokens; blocks
+  int head, skip;  // blocks from `head` on lie `skip` blocks further
+  __device__ __forceinline__ int token(int block) const { return (block < head ? block : block + skip) * kBlock; }
 };
-__device__ __forceinline__ RowSteps row_steps(const CacheAttnParams& p, int len) {
-  RowSteps r;
+__device__ __forceinline__ RowBlocks row_blocks(const CacheAttnParams& p, int len) {
+  RowBlocks r;
   r.len = len < 0 ? 0 : len < p.max_len ? len : p.max_len;
-  r.n = (r.len + kStep - 1) / kStep;
+  r.n = (r.len + kBlock - 1) / kBlock;
   r.head = r.n;
   r.skip = 0;
   if (p.W > 0) {
-    const int head = (p.S + kStep - 1) / kStep, tail = (r.len - p.W) / kStep;  // first step of the window
+    const int head = (p.S + kBlock - 1) / kBlock, tail = (r.len - p.W) / kBlock;  // first block of the window
     if (r.len > p.W && tail > head) {
       r.head = head;
       r.skip = tail - head;
@@ -37,116 +43,126 @@ __device__ __forceinline__ RowSteps row_steps(const CacheAttnParams& p, int len)
   }
   return r;
 }
-__device__ __forceinline__ int row_units(const CacheAttnParams& p, int len) { return (row_steps(p, len).n + p.per_unit - 1) / p.per_unit; }
+__device__ __forceinline__ int weight_of(const CacheAttnParams& p, int blocks) {
+  return blocks == 0 ? 0 : p.whole_rows ? 1 : blocks + kRowWeight;
+}
 
-// A workgroup's share of the units, [at, end), and where it begins: unit `unit` of head c of problem prob.
-struct Share {
-  int64_t at, end;
-  int prob, c, unit;
-  int total, groups;  // units in all, workgroups that have some
+// The shares: `more` of them of size + 1, the others of size.
+struct Shares {
+  int groups, size, more;
+  __device__ __forceinline__ Shares(int total, int groups_) : groups(groups_), size(total / groups_), more(total - total / groups_ * groups_) {}
+  __device__ __forceinline__ int begin(int group) const { return group * size + min(group, more); }
+  __device__ __forceinline__ int group_of(int at) const {
+    const int large = more * (size + 1);
+    return at < large ? at / (size + 1) : more + (at - large) / size;
+  }
 };
-__device__ __forceinline__ int64_t share_begin(int total, int groups, int group) { return (int64_t)total * group / groups; }
-// The workgroup that unit u belongs to.
-__device__ __forceinline__ int group_of(const Share& s, int64_t u) { return (int)(((u + 1) * s.groups - 1) / s.total); }
-__device__ __forceinline__ int units_of(const CacheAttnParams& p, int first, int n) {
-  int sum = 0;
-#pragma unroll 4
-  for (int i = 0; i < n; ++i) sum += row_units(p, p.lens[first + i]);
-  return sum;
-}
-__device__ __forceinline__ Share find_share(const CacheAttnParams& p, int group, int lane) {
-  Share s;
-  int lo = 0, n = p.P, before = 0;
-  bool counted = false;
-  for (;;) {  // a problem out of 64, of 64 * 64, ...
-    const int per = (n + 63) / 64, first = lane * per, mine = n - first < 0 ? 0 : n - first < per ? n - first : per;
-    const int incl = wave_scan_incl(units_of(p, lo + first, mine));
-    if (!counted) {
-      counted = true;
-      s.total = __builtin_amdgcn_readlane(incl, 63) * p.Hkv;
-      s.groups = s.total < p.n_groups ? s.total : p.n_groups;
-      s.at = s.end = 0;
-      s.prob = s.c = s.unit = 0;
-      if (group >= s.groups) return s;
-      s.at = share_begin(s.total, s.groups, group);
-      s.end = share_begin(s.total, s.groups, group + 1);
-    }
-    // the first lane whose problems reach beyond the share's begin
-    const int hit = __ffsll((unsigned long long)__ballot((int64_t)(before + incl) * p.Hkv > s.at)) - 1;
-    before += hit > 0 ? __builtin_amdgcn_readlane(incl, hit - 1) : 0;
-    lo += hit * per;
-    n = n - hit * per < per ? n - hit * per : per;
-    if (per == 1) break;
-  }
-  s.prob = lo;
-  const int in_problem = (int)(s.at - (int64_t)before * p.Hkv), units = row_units(p, p.lens[lo]);
-  s.c = in_problem / units;
-  s.unit = in_problem % units;
-  return s;
-}
-// Problems without tokens: out = 0, lse = -infinity.
-__device__ __forceinline__ void clear_empty(const CacheAttnParams& p) {
-  for (int prob = blockIdx.x; prob < p.P; prob += gridDim.x) {
-    if (p.lens[prob] > 0) continue;
-    for (int i = threadIdx.x; i < p.Hq * p.D; i += blockDim.x) p.out[(int64_t)prob * p.Hq * p.D + i] = 0.f;
-    if (p.lse)
-      for (int i = threadIdx.x; i < p.Hq; i += blockDim.x) p.lse[(int64_t)prob * p.Hq + i] = -INFINITY;
-  }
-}
 
 // One row's part in a workgroup.
 struct Segment {
-  int prob, c, step0, step1, units;
-  RowSteps row;
-  int64_t row_begin;  // the row's first unit
-  bool whole;         // the row is nobody else's
-  int slot;           // else: this workgroup's first or second part
+  int prob, c, block0, block1;
+  RowBlocks row;
+  int row_end;  // in weights, from the first row's beginning
+  __device__ __forceinline__ bool whole() const { return block0 == 0 && block1 == row.n; }
 };
+
 // A workgroup's rows in turn.
 struct Walk {
-  Share sh;
-  RowSteps row;
-  int64_t at;
-  int prob, c, unit, todo;
-  __device__ __forceinline__ Walk(const CacheAttnParams& p, int group, int lane) : sh(find_share(p, group, lane)) {
-    at = sh.at;
-    prob = sh.prob, c = sh.c, unit = sh.unit, todo = 0;
-    if (at < sh.end) row = row_steps(p, p.lens[prob]);
-  }
-  __device__ __forceinline__ bool more() const { return at < sh.end; }
-  __device__ __forceinline__ Segment segment(const CacheAttnParams& p) {
-    Segment g;
-    g.prob = prob, g.c = c, g.row = row;
-    g.units = (row.n + p.per_unit - 1) / p.per_unit;
-    todo = g.units - unit < sh.end - at ? g.units - unit : (int)(sh.end - at);
-    g.whole = todo == g.units;
-    g.slot = at == sh.at ? 0 : 1;
-    g.step0 = unit * p.per_unit;
-    g.step1 = min(row.n, (unit + todo) * p.per_unit);
-    g.row_begin = at - unit;
-    return g;
-  }
-  __device__ __forceinline__ void next(const CacheAttnParams& p) {
-    at += todo;
-    unit = 0;
-    if (++c < p.Hkv || at >= sh.end) return;
-    c = 0;
-    do row = row_steps(p, p.lens[++prob]);
-    while (row.n == 0 && prob + 1 < p.P);
-  }
-  // The second workgroup of a row that is not one workgroup's alone asks for its parts to be joined.
-  __device__ __forceinline__ void leave_record(const CacheAttnParams& p, const Segment& g, int group) const {
-    if (g.whole || g.slot != 0) return;
-    const int first = group_of(sh, g.row_begin);
-    if (first != group - 1) return;
-    JoinRecord r;
-    r.row = g.prob * p.Hkv + g.c;
-    r.first = first;
-    r.last = group_of(sh, g.row_begin + g.units - 1);
-    r.first_slot = g.row_begin == share_begin(sh.total, sh.groups, first) ? 0 : 1;
-    p.joins[group] = r;
+  int at, end;  // its share, in weights
+  int prob, c, done;  // the row that `at` is in, and what of its weight lies before
+  RowBlocks row;
+  // the next row's part that holds blocks; false: none is left
+  __device__ __forceinline__ bool next(const CacheAttnParams& p, Segment* g) {
+    while (at < end) {
+      const int weight = weight_of(p, row.n);
+      if (done == weight) {
+        done = 0;
+        if (++c == p.Hkv) {
+          c = 0;
+          do row = row_blocks(p, length_of(p, ++prob));
+          while (row.n == 0 && prob + 1 < p.P);
+        }
+        continue;
+      }
+      const int take = min(weight - done, end - at);
+      const int skip = p.whole_rows ? 0 : kRowWeight;
+      g->prob = prob, g->c = c, g->row = row;
+      g->row_end = at - done + weight;
+      g->block0 = max(done - skip, 0);
+      g->block1 = p.whole_rows ? row.n : max(done + take - skip, 0);
+      at += take;
+      done += take;
+      if (g->block1 > g->block0) return true;
+    }
+    return false;
   }
 };
+
+__device__ __forceinline__ int weights_of(const CacheAttnParams& p, int first, int n) {
+  int sum = 0;
+  for (int i0 = 0; i0 < n; i0 += 4) {
+    int len[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) len[i] = p.lens[first + min(i0 + i, n - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += i0 + i < n ? weight_of(p, row_blocks(p, len[i]).n) : 0;
+  }
+  return sum;
+}
+__device__ __forceinline__ void find_share(const CacheAttnParams& p, int group, int lane, Walk* w, Shares* shares) {
+  int lo = 0, n = p.P, before = 0;
+  bool counted = false;
+  for (;;) {  // a problem out of 64, of 64 * 64, ...
+    const int per = (n + 63) / 64, first = lane * per, mine = max(0, min(per, n - first));
+    const int incl = wave_scan_incl(weights_of(p, lo + first, mine)) * p.Hkv;
+    if (!counted) {
+      counted = true;
+      const int total = __builtin_amdgcn_readlane(incl, 63);
+      const int busy = p.whole_rows ? total : (total + kGroupBlocks - 1) / kGroupBlocks;
+      *shares = Shares(total, max(1, min(busy, p.n_groups)));
+      w->at = w->end = 0;
+      if (group >= shares->groups || total == 0) return;
+      w->at = shares->begin(group);
+      w->end = shares->begin(group + 1);
+    }
+    // the first lane whose problems reach beyond the share's begin
+    const int hit = __ffsll((unsigned long long)__ballot(before + incl > w->at)) - 1;
+    before += hit > 0 ? __builtin_amdgcn_readlane(incl, hit - 1) : 0;
+    lo += hit * per;
+    n = min(per, n - hit * per);
+    if (per == 1) break;
+  }
+  w->prob = lo;
+  w->row = row_blocks(p, length_of(p, lo));
+  const int weight = weight_of(p, w->row.n), in_problem = w->at - before;
+  w->c = in_problem / weight;
+  w->done = in_problem - w->c * weight;
+}
+
+// Where a row's parts lie, left by the workgroup that begins the row: a record per row (of rows without tokens by clear_empty), or, where there
+// are more rows than workgroups, one per workgroup, which begins one row at most that it does not end.
+__device__ __forceinline__ void leave_record(const CacheAttnParams& p, const Shares& shares, const Segment& g, int group) {
+  const int row = g.prob * p.Hkv + g.c;
+  if (g.block0 != 0 || (g.whole() && !p.by_row)) return;
+  JoinRecord r = {row, -1, 0};
+  if (!g.whole()) {
+    r.first = group;
+    r.last = shares.group_of(g.row_end - 1);
+  }
+  p.joins[p.by_row ? row : group] = r;
+}
+
+// Problems without tokens: out = 0, lse = -infinity.
+__device__ __forceinline__ void clear_empty(const CacheAttnParams& p) {
+  for (int prob = blockIdx.x; prob < p.P; prob += gridDim.x) {
+    if (length_of(p, prob) > 0) continue;
+    for (int i = threadIdx.x; i < p.Hq * p.D; i += blockDim.x) p.out[(int64_t)prob * p.Hq * p.D + i] = 0.f;
+    if (p.lse)
+      for (int i = threadIdx.x; i < p.Hq; i += blockDim.x) p.lse[(int64_t)prob * p.Hq + i] = -INFINITY;
+    if (p.by_row)
+      for (int c = threadIdx.x; c < p.Hkv; c += blockDim.x) p.joins[prob * p.Hkv + c].first = -1;
+  }
+}
 
 // Tokens of a row that are attended; a block of n tokens from t0 on: are there any that are not?
 struct Mask {
@@ -156,14 +172,66 @@ struct Mask {
   __device__ __forceinline__ bool cuts(int t0, int n) const { return t0 + n > len || (tail > t0 && t0 + n > S); }
 };
 
-// Merges the parts of a row that were left in scratch: a workgroup per (share boundary, head).
+// Loads of a wave, in the order of its blocks, segment after segment: its it-th block of a segment is the segment's block
+// wave + NW * it.  They run a block ahead of the arithmetic, into the next row's first block too: the merge of a row's waves would otherwise leave the memory idle.
+template <int D, int NW>
+struct BlockLoads {
+  static constexpr int CH = D / 8, TPL = 64 / CH, NLOAD = kBlock / TPL;
+  Walk walk;
+  RowBlocks row;
+  int wave, lane, prob, c, first, n, it;
+  int pages;  // of the next 64 groups of 16 tokens, one per lane (a dense cache's "page" is the problem)
+  bool valid;
+  __device__ __forceinline__ BlockLoads(const CacheAttnParams& p, const Walk& w, int wave_, int lane_)
+      : walk(w), wave(wave_), lane(lane_), n(0), it(-1), valid(true) {
+    step(p);
+  }
+  // to the next block; valid: there is one
+  __device__ __forceinline__ void step(const CacheAttnParams& p) {
+    ++it;
+    while (it >= n) {
+      Segment g;
+      valid = walk.next(p, &g);
+      if (!valid) return;
+      row = g.row, prob = g.prob, c = g.c;
+      first = g.block0 + wave;
+      n = g.block1 > first ? (g.block1 - first + NW - 1) / NW : 0;
+      it = 0;
+    }
+    if ((it & 31) != 0) return;
+    pages = prob;
+    if (!p.cache.table) return;
+    const int t = min(row.token(first + min(it + (lane >> 1), n - 1) * NW) + (lane & 1) * 16, row.len - 1);
+    const int page = p.cache.table[(int64_t)prob * p.cache.pitch + (t >> p.cache.shift)];
+    pages = page < 0 ? 0 : page >= p.cache.n_blocks ? p.cache.n_blocks - 1 : page;
+  }
+  // Tokens behind the row are its last one again.
+  __device__ __forceinline__ void load(const CacheAttnParams& p, const char* base, int64_t s_block, int64_t s_head, int64_t s_token, uint4 (&dst)[NLOAD]) const {
+    const int t0 = row.token(first + it * NW), in_block = (int)((1u << p.cache.shift) - 1u);
+    base += c * s_head;
+#pragma unroll
+    for (int i = 0; i < NLOAD; ++i) {
+      const char* b = base + (int64_t)__builtin_amdgcn_readlane(pages, (it * 2 + i * TPL / 16) & 63) * s_block;
+      const int t = min(t0 + i * TPL + lane / CH, row.len - 1) & in_block;
+      dst[i] = ld16_stream(b + t * s_token + lane % CH * 16);
+    }
+  }
+  __device__ __forceinline__ void load_k(const CacheAttnParams& p, uint4 (&dst)[NLOAD]) const {
+    load(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, dst);
+  }
+  __device__ __forceinline__ void load_v(const CacheAttnParams& p, uint4 (&dst)[NLOAD]) const {
+    load(p, p.cache.V, p.cache.vs_block, p.cache.vs_head, p.cache.vs_token, dst);
+  }
+};
+
+// Merges the parts of a row that were left in scratch: a workgroup per (record, head).
 __global__ __launch_bounds__(128) void join_kernel(CacheAttnParams p) {
   const JoinRecord r = p.joins[blockIdx.x];
   if (r.first < 0) return;
   const int g = blockIdx.y, j = threadIdx.x, sl = threadIdx.x & 31;
   if (j >= p.D) return;  // wave-uniform
   const int n = r.last - r.first + 1;
-  auto part = [&](int s) { return ((int64_t)(r.first + s) * 2 + (s == 0 ? r.first_slot : 0)) * p.G + g; };
+  auto part = [&](int s) { return ((int64_t)(r.first + s) * 2 + (s == 0)) * p.G + g; };
   float M = -INFINITY, num = 0.f;
   double den = 0.0;
   const float c = p.join_scale * 1.44269502162933349609375f;
@@ -189,12 +257,12 @@ __global__ __launch_bounds__(128) void join_kernel(CacheAttnParams p) {
   if (p.lse && j == 0) p.lse[head] = den == 0.0 ? -INFINITY : fmaf(M, p.join_scale, logf((float)den));
 }
 
-// bf16 caches.  Per wave a block of 32 tokens of the step: K goes through the wave's staging buffer in LDS (16-byte chunks, XOR-swizzled) into
+// bf16 caches.  A wave takes 32 tokens at a time: K goes through the wave's staging buffer in LDS (16-byte chunks, XOR-swizzled) into
 // v_mfma_f32_16x16x32_bf16 with the queries as the A operand, their rows repeated, so that a lane takes the tile of its slot and ends
 // with 4 logits of one token; V goes through the same buffer and is read transposed (ds_read_b64_tr_b16).  A softmax weight, fp32, is cut into three bf16
 // parts of 8 bits each, which add up to it exactly: rows of the second product's A operand that the group's heads leave free take them, so up to four heads
 // cost one product as they would with weights rounded to bf16, eight two, sixteen three.  (Rounded to bf16 the weights would put the outputs 1e-3 off, fp32's
-// own error is 1e-6, and the matrix cores have nothing else to do: one step's 128 tokens of 128 dims are 64 KB, 2.5 us of HBM time for a CU.)
+// own error is 1e-6, and the matrix cores have nothing else to do: four blocks of 128 dims are 64 KB, 2.5 us of HBM time for a CU.)
 template <int D, int GPAD>
 __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
   constexpr int BT = 32, NW = 4;
@@ -213,9 +281,13 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
   const int n = lane & 15, j = lane >> 4;    // MFMA role: column, row block / k-group
   const int group = blockIdx.x, g0 = p.g0, gb = p.gb;
   if (g0 == 0) clear_empty(p);
-  Walk walk(p, group, lane);
-  if (tid == 0) p.joins[group].first = -1;
-  if (!walk.more()) return;
+  if (tid == 0 && !p.by_row) p.joins[group].first = -1;
+  Walk walk;
+  Shares shares(0, 1);
+  find_share(p, group, lane, &walk, &shares);
+  BlockLoads<D, NW> ahead(p, walk, wave, lane);
+  Segment seg;
+  if (!walk.next(p, &seg)) return;
 
   uint4* buf = kbuf[wave];
 #pragma unroll
@@ -224,54 +296,23 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
   const float cexp = p.scale * 1.44269502162933349609375f;
   auto vswz = [](int t) { return CH == 16 ? (((t & 3) << 1) | (((t >> 3) & 1) << 3)) : ((t & 3) << 1); };
 
-  for (; walk.more(); walk.next(p)) {
-    const Segment seg = walk.segment(p);
-    const RowSteps row = seg.row;
-    const int prob = seg.prob, c = seg.c;
-    const Mask mask(p, row.len);
-    // this wave's blocks: one in each step, none in the row's last one if that ends before
-    auto token0 = [&](int it) { return row.token(seg.step0 + it) + wave * BT; };
-    int nblk = seg.step1 - seg.step0;
-    if (token0(nblk - 1) >= row.len) --nblk;
-
-    uint4 qa[KSTEPS];
-    {
-      const char* qrow = p.q + (((int64_t)prob * p.Hq + c * p.G + g0 + n % GPAD) * D + 8 * j) * 2;
+  uint4 kv[NLOAD], vv[NLOAD], qa[KSTEPS];
+  auto load_q = [&](int prob, int c) {
+    const char* qrow = p.q + (((int64_t)prob * p.Hq + c * p.G + g0 + n % GPAD) * D + 8 * j) * 2;
 #pragma unroll
-      for (int kc = 0; kc < KSTEPS; ++kc) {
-        qa[kc] = make_uint4(0u, 0u, 0u, 0u);
-        if (n % GPAD < gb) qa[kc] = ld16(qrow + 64 * kc);
-      }
+    for (int kc = 0; kc < KSTEPS; ++kc) {
+      qa[kc] = make_uint4(0u, 0u, 0u, 0u);
+      if (n % GPAD < gb) qa[kc] = ld16(qrow + 64 * kc);
     }
-    const char* Kb = p.cache.K + c * p.cache.ks_head;
-    const char* Vb = p.cache.V + c * p.cache.vs_head;
-    const int32_t* tab = p.cache.table ? p.cache.table + (int64_t)prob * p.cache.pitch : nullptr;
-    const int in_block = (int)((1u << p.cache.shift) - 1u);
-    int my_block = prob;  // paged: pages of the wave's next 64 groups of 16 tokens, one per lane
-    auto fill = [&](int it0) {
-      if (!tab) return;
-      const int it = min(it0 + (lane >> 1), nblk - 1);
-      const int t = min(token0(it) + (lane & 1) * 16, row.len - 1);
-      const int b = tab[t >> p.cache.shift];
-      my_block = b < 0 ? 0 : b >= p.cache.n_blocks ? p.cache.n_blocks - 1 : b;
-    };
-    auto load = [&](int it, const char* base, int64_t s_block, int64_t s_token, uint4 (&dst)[NLOAD]) {
-      const int t0 = token0(it);
-      const bool full = t0 + BT <= row.len;  // wave-uniform
-#pragma unroll
-      for (int i = 0; i < NLOAD; ++i) {
-        const int t = t0 + i * TPL;
-        const char* b = base + (int64_t)__builtin_amdgcn_readlane(my_block, (it * 2 + i * TPL / 16) & 63) * s_block;
-        const int tl = full ? (t & in_block) + tq : min(t + tq, row.len - 1) & in_block;
-        dst[i] = ld16_stream(b + tl * s_token + cl * 16);
-      }
-    };
-    uint4 kv[NLOAD], vv[NLOAD];
-    if (nblk > 0) {
-      fill(0);
-      load(0, Kb, p.cache.ks_block, p.cache.ks_token, kv);
-      load(0, Vb, p.cache.vs_block, p.cache.vs_token, vv);
-    }
+  };
+  load_q(seg.prob, seg.c);
+  if (ahead.valid) {
+    ahead.load_k(p, kv);
+    ahead.load_v(p, vv);
+  }
+  for (;;) {
+    const Mask mask(p, seg.row.len);
+    const int first = seg.block0 + wave, nblk = seg.block1 > first ? (seg.block1 - first + NW - 1) / NW : 0;
 
     float m_run[4], l_part[4];
 #pragma unroll
@@ -281,7 +322,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
     for (int nd = 0; nd < NDT; ++nd) acc[nd] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
     for (int it = 0; it < nblk; ++it) {
-      const int t0 = token0(it);
+      const int t0 = seg.row.token(first + it * NW);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of the buffer are done
 #pragma unroll
       for (int i = 0; i < NLOAD; ++i) {
@@ -289,17 +330,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
         buf[t * CH + (cl ^ (t & (CH - 1)))] = kv[i];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      const bool more = it + 1 < nblk;
       const bool cut = mask.cuts(t0, BT);  // wave-uniform: some of the block's tokens are not attended
       if (cut) {  // V of those is not to be looked at
 #pragma unroll
         for (int i = 0; i < NLOAD; ++i)
           if (!mask.at(t0 + i * TPL + tq)) vv[i] = make_uint4(0u, 0u, 0u, 0u);
       }
-      if (more) {
-        if (((it + 1) & 31) == 0) fill(it + 1);  // (V of the present block is on its way already)
-        load(it + 1, Kb, p.cache.ks_block, p.cache.ks_token, kv);
-      }
+      ahead.step(p);  // (V of the present block is on its way already)
+      if (ahead.valid) ahead.load_k(p, kv);
 
       float x[NACC][4];
 #pragma unroll
@@ -367,7 +405,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
         buf[t * CH + (cl ^ vswz(t))] = vv[i];
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (more) load(it + 1, Vb, p.cache.vs_block, p.cache.vs_token, vv);
+      if (ahead.valid) ahead.load_v(p, vv);
 
       uint4 pa[NSET];
 #pragma unroll
@@ -393,6 +431,9 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
       }
     }
 
+    Segment next;
+    const bool more = walk.next(p, &next);
+    if (more) load_q(next.prob, next.c);
     // the wave's totals: weights over the lanes that share a head, accumulators over the rows that hold its parts
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -418,7 +459,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
     __syncthreads();
     constexpr int kAccStride = BT * ROWB / 4;  // floats between the waves' buffers
     const float* all = reinterpret_cast<const float*>(&kbuf[0][0]);
-    const int64_t part = ((int64_t)group * 2 + seg.slot) * p.G + g0, head0 = ((int64_t)prob * p.Hkv + c) * p.G + g0;
+    const int64_t part = ((int64_t)group * 2 + (seg.block0 == 0)) * p.G + g0, head0 = ((int64_t)seg.prob * p.Hkv + seg.c) * p.G + g0;
 #pragma unroll
     for (int i0 = 0; i0 < GPAD * D; i0 += NW * 64) {
       const int g = (i0 + tid) / D, jj = tid % D;
@@ -437,7 +478,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
         a += ml[w].x == -INFINITY ? 0.f : all[w * kAccStride + g * D + jj] * f;
         ls += ml[w].y * f;
       }
-      if (seg.whole) {
+      if (seg.whole()) {
         p.out[(head0 + g) * D + jj] = ls == 0.f ? 0.f : a / ls;
         if (p.lse && jj == 0) p.lse[head0 + g] = ls == 0.f ? -INFINITY : fmaf(M, p.scale, logf(ls));
       } else {
@@ -445,18 +486,20 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
         if (jj == 0) p.part_ml[part + g] = make_float2(M, ls);
       }
     }
-    if (tid == 0) walk.leave_record(p, seg, group);
+    if (tid == 0) leave_record(p, shares, seg, group);
+    if (!more) return;
     __syncthreads();  // buffers and s_ml are free again
+    seg = next;
   }
 }
 
 // fp32 caches.  Both products and the sums in fp64 (an fp32 logit of magnitude 100 would be off by 2.5e-5, and so would its softmax weight);
 // fp64 and fp32 multiply-adds take the same four cycles.  Eight lanes share a token, a logit's eight parts are summed while
 // heads and lanes change places, and lane s of the eight ends with head s's logit, whose weight it computes once and leaves in LDS for the lanes that
-// hold V's chunks.  GB heads, at most 8; a step of 128 tokens is a block for each of the workgroup's waves.
+// hold V's chunks.  GB heads, at most 8.
 template <int D, int GB>
 __global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(CacheAttnParams p) {
-  constexpr int NW = D == 128 ? 8 : 4, BT = kStep / NW, kThreads = NW * 64;
+  constexpr int NW = D == 128 ? 8 : 4, BT = kBlock * kGroupBlocks / NW, kThreads = NW * 64;
   constexpr int CH = D / 4, GPB = BT / 16;
   constexpr bool LATE_V = GB >= 4;             // V's block after the logits, not with K's: else registers spill
   constexpr int NG = BT / 8, NC = CH / 8;      // K: groups of 8 tokens, a lane's chunks of a token
@@ -473,18 +516,21 @@ __global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(Ca
   const int tq = lane / CH, cl = lane % CH;  // V role: token of a load, chunk
   const int group = blockIdx.x, g0 = p.g0;
   if (g0 == 0) clear_empty(p);
-  Walk walk(p, group, lane);
-  if (tid == 0) p.joins[group].first = -1;
+  if (tid == 0 && !p.by_row) p.joins[group].first = -1;
+  Walk walk;
+  Shares shares(0, 1);
+  find_share(p, group, lane, &walk, &shares);
 
-  for (; walk.more(); walk.next(p)) {
-    const Segment seg = walk.segment(p);
-    const RowSteps row = seg.row;
+  for (Segment seg; walk.next(p, &seg);) {
+    const RowBlocks row = seg.row;
     const int prob = seg.prob, c = seg.c;
     const Mask mask(p, row.len);
     const int64_t head0 = ((int64_t)prob * p.Hkv + c) * p.G + g0;
-    auto token0 = [&](int it) { return row.token(seg.step0 + it) + wave * BT; };
-    int nblk = seg.step1 - seg.step0;
-    if (token0(nblk - 1) >= row.len) --nblk;
+    // 128 dims: two waves share a block
+    constexpr int SHARE = kBlock / BT;
+    auto token0 = [&](int it) { return row.token(seg.block0 + wave / SHARE + it * kGroupBlocks) + wave % SHARE * BT; };
+    int nblk = (seg.block1 - seg.block0 - wave / SHARE + kGroupBlocks - 1) / kGroupBlocks;
+    if (nblk > 0 && token0(nblk - 1) >= row.len) --nblk;
 
     const char* Kb = p.cache.K + c * p.cache.ks_head;
     const char* Vb = p.cache.V + c * p.cache.vs_head;
@@ -645,7 +691,7 @@ __global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(Ca
       s_l[wave][lane] = l;
     }
     __syncthreads();
-    const int64_t part = ((int64_t)group * 2 + seg.slot) * p.G + g0;
+    const int64_t part = ((int64_t)group * 2 + (seg.block0 == 0)) * p.G + g0;
     for (int i = tid; i < GB * D; i += kThreads) {
       const int g = i / D, jj = i % D;
       float M = s_m[0][g];
@@ -658,7 +704,7 @@ __global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(Ca
         a += s_m[w][g] == -INFINITY ? 0.0 : (double)s_acc[w][g][jj] * f;
         ls += s_l[w][g] * f;
       }
-      if (seg.whole) {
+      if (seg.whole()) {
         p.out[(head0 + g) * D + jj] = ls == 0.0 ? 0.f : (float)(a / ls);
         if (p.lse && jj == 0) p.lse[head0 + g] = ls == 0.0 ? -INFINITY : (float)((double)M + log(ls));
       } else {
@@ -666,7 +712,7 @@ __global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(Ca
         if (jj == 0) p.part_ml[part + g] = make_float2(M, (float)ls);
       }
     }
-    if (tid == 0) walk.leave_record(p, seg, group);
+    if (tid == 0) leave_record(p, shares, seg, group);
     __syncthreads();  // LDS is free again
   }
 }
@@ -700,7 +746,7 @@ hipError_t launch_cache_attn(const CacheAttnParams& p, bool join, hipStream_t s)
     if (e != hipSuccess) return e;
   }
   if (!join) return hipSuccess;
-  hipLaunchKernelGGL(join_kernel, dim3((unsigned)p.n_groups, (unsigned)p.G), dim3(128), 0, s, p);
+  hipLaunchKernelGGL(join_kernel, dim3((unsigned)(p.by_row ? p.P * p.Hkv : p.n_groups), (unsigned)p.G), dim3(128), 0, s, p);
   return hipGetLastError();
 }
 

@@ -33,12 +33,14 @@ struct RotaryParams {
 };
 hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
 
-constexpr int kStep = 128;      // tokens the four waves of an attention workgroup take at a time
-constexpr int kAttnGroups = 512;  // workgroups of an attention launch at most
+constexpr int kBlock = 32;         // tokens of a row that a wave takes at a time
+constexpr int kAttnGroups = 512;   // workgroups of an attention launch at most: two per CU
+constexpr int kGroupBlocks = 4;    // blocks a workgroup has work for at a time
+constexpr int kRowWeight = 8;      // a row's beginning and end, in blocks
 
-// Where a workgroup's first row, if it began in an earlier workgroup, is to be joined: see cache_attn.hip.
+// A row whose parts are to be joined, those of workgroups first (its second slot) and first + 1 .. last (their first slots).
 struct JoinRecord {
-  int row, first, last, first_slot;  // first < 0: nothing to do
+  int row, first, last;  // first < 0: nothing to do
 };
 
 struct CacheAttnParams {
@@ -48,14 +50,15 @@ struct CacheAttnParams {
   const int32_t* lens;
   int P, Hq, Hkv, G, D, dtype;
   int S, W, max_len;
-  int per_unit;  // steps of a unit of work; a unit is never split
-  int n_groups;  // workgroups
+  bool whole_rows;  // rows are short and never split
+  bool by_row;      // a join record per row, else one per workgroup
+  int n_groups;     // workgroups
   int g0, gb;    // the group's heads that a launch handles
   float scale;       // 1 / sqrt(head_dim)
   float join_scale;  // the parts' maxima times this are logits: scale where they are products (bf16), 1 where they are logits (fp32)
   float* part_acc;    // [n_groups][2][G][D]
   float2* part_ml;    // [n_groups][2][G]
-  JoinRecord* joins;  // [n_groups]
+  JoinRecord* joins;  // [kAttnGroups]
 };
 hipError_t launch_cache_attn(const CacheAttnParams& p, bool join, hipStream_t s);
 
