@@ -270,22 +270,24 @@ sagekv_status sagekvc_attn(const sagekvc_desc* d, const sagekv_paged_kv* pages, 
   p.scale = (float)(1.0 / sqrt((double)d->head_dim));
   p.join_scale = d->dtype == SAGEKV_BF16 ? p.scale : 1.f;
   // blocks of the longest row: all of its tokens, or those of the window's two ends
-  int64_t blocks = ((int64_t)max_len + kBlock - 1) / kBlock;
+  const int bt = attn_block(d->dtype, d->head_dim);
+  int64_t blocks = ((int64_t)max_len + bt - 1) / bt;
   if (p.W > 0) {
-    const int64_t ends = (p.S + kBlock - 1) / kBlock + (p.W + kBlock - 2) / kBlock + 1;
+    const int64_t ends = (p.S + bt - 1) / bt + (p.W + bt - 2) / bt + 1;
     if (ends < blocks) blocks = ends;
   }
-  // up to two rounds of a workgroup's waves: rows are left whole, and there is nothing to join
-  p.whole_rows = blocks <= 2 * kGroupBlocks;
-  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads, weight = rows * (p.whole_rows ? 1 : blocks + kRowWeight);
-  if (weight > 0x7FFFFFFF - kGroupBlocks) return SAGEKV_ERR_UNSUPPORTED;
-  const int64_t busy = p.whole_rows ? weight : (weight + kGroupBlocks - 1) / kGroupBlocks;
-  p.n_groups = busy < kAttnGroups ? (int)busy : kAttnGroups;
+  // Rows of up to 256 tokens are not worth a join: a workgroup's four waves take a row together, or, where there are more rows than workgroups, a wave
+  // takes it alone.
+  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads;
+  p.row_parts = blocks * bt > 256 ? 0 : rows <= kAttnGroups ? 4 : 1;
+  const int64_t weight = rows * (p.row_parts ? p.row_parts : blocks + kRowWeight);
+  if (weight > 0x7FFFFFFF) return SAGEKV_ERR_UNSUPPORTED;
+  p.n_waves = weight < kAttnWaves ? (int)weight : kAttnWaves;
   p.by_row = rows <= kAttnGroups;
   p.part_acc = (float*)((char*)workspace + l.acc);
   p.part_ml = (float2*)((char*)workspace + l.ml);
   p.joins = (JoinRecord*)((char*)workspace + l.joins);
-  return dev(launch_cache_attn(p, !p.whole_rows, (hipStream_t)hip_stream));
+  return dev(launch_cache_attn(p, p.row_parts == 0, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

@@ -1,10 +1,14 @@
 // Attention of one new token per sequence over the full cache, every sequence of its own length.
 //
-// A row (sequence, KV head) is cut into blocks of 32 tokens.  All rows, one after the other, are divided over the launch's workgroups, whatever their
-// lengths: a row weighs its blocks and kRowWeight more for its beginning and end, and every workgroup gets the same weight.  It finds its share from the
-// lengths alone, which it reads on the device (64 of them at a time, summed over the wave).  A row that one workgroup has for itself is written straight
-// to `out`; parts of a row shared by several go to scratch, at most two a workgroup: one that continues a row and one that begins
-// one.  join_kernel merges them, (max, sum, accumulator) by (max, sum, accumulator).
+// A row (sequence, KV head) is cut into blocks of 32 tokens (fp32, 128 dims: 16), a wave's work at a time.  All rows, one after the other, are divided
+// over the launch's waves, whatever their lengths: a row weighs its blocks and kRowWeight more for its beginning and end, and every wave gets the same
+// weight, a run of blocks that may hold several rows and two parts of rows at most, one that continues a row and one that begins
+// one.  A wave finds its share from the lengths alone, which it reads on the device (64 of them at a time, summed over the wave), and goes through it without waiting for
+// any other: its loads run a block ahead of its arithmetic, into the next row too.  A whole row goes straight to `out`; parts stay in LDS until the
+// four waves of the workgroup, whose shares are neighbours, are done, and are merged there, (max, sum, accumulator) by (max, sum, accumulator).  What the
+// workgroup then has not got the whole of goes to scratch, one row that it continues and one that it begins at most, and join_kernel merges that.
+// (With shares for workgroups, whose four waves took a row's blocks in turn and merged them at its end, a row cost as much as 8 blocks, and 64 sequences of
+// 1 to 32K tokens 88 us.)
 //
 // Bound by HBM: K and V are read once, for all heads of the group at a time.
 #include "device_utils.h"
@@ -14,6 +18,8 @@ namespace sagekv {
 
 namespace {
 
+constexpr int NW = 4;  // waves of a workgroup
+
 // ---- rows, weights and shares ------------------------------------------------------------------
 // Lengths do not change while a launch runs: through the constant address space they come by scalar loads, which nothing else waits for.  (A vector
 // load of a length in the middle of a share waits for all of K and V that is in flight.)
@@ -22,74 +28,126 @@ __device__ __forceinline__ int length_of(const CacheAttnParams& p, int prob) {
 }
 
 // The blocks of a row of len tokens that hold attended tokens.  With a window those of the first S and of the last W tokens.
+template <int BT>
 struct RowBlocks {
   int len, n;      // tokens; blocks
   int head, skip;  // blocks from `head` on lie `skip` blocks further
-  __device__ __forceinline__ int token(int block) const { return (block < head ? block : block + skip) * kBlock; }
-};
-__device__ __forceinline__ RowBlocks row_blocks(const CacheAttnParams& p, int len) {
-  RowBlocks r;
-  r.len = len < 0 ? 0 : len < p.max_len ? len : p.max_len;
-  r.n = (r.len + kBlock - 1) / kBlock;
-  r.head = r.n;
-  r.skip = 0;
-  if (p.W > 0) {
-    const int head = (p.S + kBlock - 1) / kBlock, tail = (r.len - p.W) / kBlock;  // first block of the window
-    if (r.len > p.W && tail > head) {
-      r.head = head;
-      r.skip = tail - head;
-      r.n -= r.skip;
+  __device__ __forceinline__ int token(int block) const { return (block < head ? block : block + skip) * BT; }
+  __device__ __forceinline__ RowBlocks() {}
+  __device__ __forceinline__ RowBlocks(const CacheAttnParams& p, int length) {
+    len = length < 0 ? 0 : length < p.max_len ? length : p.max_len;
+    n = (len + BT - 1) / BT;
+    head = n;
+    skip = 0;
+    if (p.W > 0) {
+      const int sinks = (p.S + BT - 1) / BT, tail = (len - p.W) / BT;  // blocks of the sink tokens, first block of the window
+      if (len > p.W && tail > sinks) {
+        head = sinks;
+        skip = tail - sinks;
+        n -= skip;
+      }
     }
   }
-  return r;
-}
+};
 __device__ __forceinline__ int weight_of(const CacheAttnParams& p, int blocks) {
-  return blocks == 0 ? 0 : p.whole_rows ? 1 : blocks + kRowWeight;
+  return blocks == 0 ? 0 : p.row_parts ? p.row_parts : blocks + kRowWeight;
 }
 
 // The shares: `more` of them of size + 1, the others of size.
 struct Shares {
-  int groups, size, more;
-  __device__ __forceinline__ Shares(int total, int groups_) : groups(groups_), size(total / groups_), more(total - total / groups_ * groups_) {}
-  __device__ __forceinline__ int begin(int group) const { return group * size + min(group, more); }
-  __device__ __forceinline__ int group_of(int at) const {
+  int n, size, more;
+  __device__ __forceinline__ Shares(int total, int n_) : n(n_), size(total / n_), more(total - total / n_ * n_) {}
+  __device__ __forceinline__ int begin(int i) const { return i * size + min(i, more); }
+  __device__ __forceinline__ int of(int at) const {
     const int large = more * (size + 1);
     return at < large ? at / (size + 1) : more + (at - large) / size;
   }
 };
 
-// One row's part in a workgroup.
-struct Segment {
+// A part of a row, blocks [block0, block1).
+template <int BT>
+struct Part {
   int prob, c, block0, block1;
-  RowBlocks row;
+  RowBlocks<BT> row;
   int row_end;  // in weights, from the first row's beginning
-  __device__ __forceinline__ bool whole() const { return block0 == 0 && block1 == row.n; }
 };
 
-// A workgroup's rows in turn.
+// Weight of n problems (of a row of each); *one: the length, if it is one.
+template <int BT>
+__device__ __forceinline__ int weights_of(const CacheAttnParams& p, int first, int n, int* one) {
+  int sum = 0;
+  for (int i0 = 0; i0 < n; i0 += 4) {
+    int len[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) len[i] = p.lens[first + min(i0 + i, n - 1)];
+    *one = len[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += i0 + i < n ? weight_of(p, RowBlocks<BT>(p, len[i]).n) : 0;
+  }
+  return sum;
+}
+
+// A wave's share, part by part.
+template <int BT>
 struct Walk {
-  int at, end;  // its share, in weights
+  int at, end;        // what is left of it, in weights
   int prob, c, done;  // the row that `at` is in, and what of its weight lies before
-  RowBlocks row;
-  // the next row's part that holds blocks; false: none is left
-  __device__ __forceinline__ bool next(const CacheAttnParams& p, Segment* g) {
+  RowBlocks<BT> row;
+  // wave: its number in the launch
+  __device__ __forceinline__ Shares start(const CacheAttnParams& p, int wave, int lane) {
+    int lo = 0, n = p.P, before = 0, length = 0;
+    Shares shares(0, 1);
+    bool counted = false;
+    at = end = 0;
+    for (;;) {  // a problem out of 64, of 64 * 64, ...
+      const int per = (n + 63) / 64, first = lane * per, mine = max(0, min(per, n - first));
+      const int incl = wave_scan_incl(weights_of<BT>(p, lo + first, mine, &length)) * p.Hkv;
+      if (!counted) {
+        counted = true;
+        const int total = __builtin_amdgcn_readlane(incl, 63);
+        shares = Shares(total, max(1, min(total, p.n_waves)));
+        if (wave >= min(total, p.n_waves)) return shares;
+        at = shares.begin(wave);
+        end = shares.begin(wave + 1);
+      }
+      // the first lane whose problems reach beyond the share's begin
+      const int hit = __ffsll((unsigned long long)__ballot(before + incl > at)) - 1;
+      before += hit > 0 ? __builtin_amdgcn_readlane(incl, hit - 1) : 0;
+      lo += hit * per;
+      n = min(per, n - hit * per);
+      if (per > 1) continue;
+      row = RowBlocks<BT>(p, __builtin_amdgcn_readlane(length, hit));
+      break;
+    }
+    prob = lo;
+    const int weight = weight_of(p, row.n), in_problem = at - before;
+    c = in_problem / weight;
+    done = in_problem - c * weight;
+    return shares;
+  }
+  // the next part that holds blocks; false: none is left
+  __device__ __forceinline__ bool next(const CacheAttnParams& p, Part<BT>* g) {
     while (at < end) {
       const int weight = weight_of(p, row.n);
       if (done == weight) {
         done = 0;
         if (++c == p.Hkv) {
           c = 0;
-          do row = row_blocks(p, length_of(p, ++prob));
+          do row = RowBlocks<BT>(p, length_of(p, ++prob));
           while (row.n == 0 && prob + 1 < p.P);
         }
         continue;
       }
       const int take = min(weight - done, end - at);
-      const int skip = p.whole_rows ? 0 : kRowWeight;
       g->prob = prob, g->c = c, g->row = row;
       g->row_end = at - done + weight;
-      g->block0 = max(done - skip, 0);
-      g->block1 = p.whole_rows ? row.n : max(done + take - skip, 0);
+      if (p.row_parts) {
+        g->block0 = row.n * done / p.row_parts;
+        g->block1 = row.n * (done + take) / p.row_parts;
+      } else {
+        g->block0 = max(done - kRowWeight, 0);
+        g->block1 = max(done + take - kRowWeight, 0);
+      }
       at += take;
       done += take;
       if (g->block1 > g->block0) return true;
@@ -97,60 +155,6 @@ struct Walk {
     return false;
   }
 };
-
-__device__ __forceinline__ int weights_of(const CacheAttnParams& p, int first, int n) {
-  int sum = 0;
-  for (int i0 = 0; i0 < n; i0 += 4) {
-    int len[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) len[i] = p.lens[first + min(i0 + i, n - 1)];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum += i0 + i < n ? weight_of(p, row_blocks(p, len[i]).n) : 0;
-  }
-  return sum;
-}
-__device__ __forceinline__ void find_share(const CacheAttnParams& p, int group, int lane, Walk* w, Shares* shares) {
-  int lo = 0, n = p.P, before = 0;
-  bool counted = false;
-  for (;;) {  // a problem out of 64, of 64 * 64, ...
-    const int per = (n + 63) / 64, first = lane * per, mine = max(0, min(per, n - first));
-    const int incl = wave_scan_incl(weights_of(p, lo + first, mine)) * p.Hkv;
-    if (!counted) {
-      counted = true;
-      const int total = __builtin_amdgcn_readlane(incl, 63);
-      const int busy = p.whole_rows ? total : (total + kGroupBlocks - 1) / kGroupBlocks;
-      *shares = Shares(total, max(1, min(busy, p.n_groups)));
-      w->at = w->end = 0;
-      if (group >= shares->groups || total == 0) return;
-      w->at = shares->begin(group);
-      w->end = shares->begin(group + 1);
-    }
-    // the first lane whose problems reach beyond the share's begin
-    const int hit = __ffsll((unsigned long long)__ballot(before + incl > w->at)) - 1;
-    before += hit > 0 ? __builtin_amdgcn_readlane(incl, hit - 1) : 0;
-    lo += hit * per;
-    n = min(per, n - hit * per);
-    if (per == 1) break;
-  }
-  w->prob = lo;
-  w->row = row_blocks(p, length_of(p, lo));
-  const int weight = weight_of(p, w->row.n), in_problem = w->at - before;
-  w->c = in_problem / weight;
-  w->done = in_problem - w->c * weight;
-}
-
-// Where a row's parts lie, left by the workgroup that begins the row: a record per row (of rows without tokens by clear_empty), or, where there
-// are more rows than workgroups, one per workgroup, which begins one row at most that it does not end.
-__device__ __forceinline__ void leave_record(const CacheAttnParams& p, const Shares& shares, const Segment& g, int group) {
-  const int row = g.prob * p.Hkv + g.c;
-  if (g.block0 != 0 || (g.whole() && !p.by_row)) return;
-  JoinRecord r = {row, -1, 0};
-  if (!g.whole()) {
-    r.first = group;
-    r.last = shares.group_of(g.row_end - 1);
-  }
-  p.joins[p.by_row ? row : group] = r;
-}
 
 // Problems without tokens: out = 0, lse = -infinity.
 __device__ __forceinline__ void clear_empty(const CacheAttnParams& p) {
@@ -172,89 +176,192 @@ struct Mask {
   __device__ __forceinline__ bool cuts(int t0, int n) const { return t0 + n > len || (tail > t0 && t0 + n > S); }
 };
 
-// Loads of a wave, in the order of its blocks, segment after segment: its it-th block of a segment is the segment's block
-// wave + NW * it.  They run a block ahead of the arithmetic, into the next row's first block too: the merge of a row's waves would otherwise leave the memory idle.
-template <int D, int NW>
-struct BlockLoads {
-  static constexpr int CH = D / 8, TPL = 64 / CH, NLOAD = kBlock / TPL;
-  Walk walk;
-  RowBlocks row;
-  int wave, lane, prob, c, first, n, it;
-  int pages;  // of the next 64 groups of 16 tokens, one per lane (a dense cache's "page" is the problem)
-  bool valid;
-  __device__ __forceinline__ BlockLoads(const CacheAttnParams& p, const Walk& w, int wave_, int lane_)
-      : walk(w), wave(wave_), lane(lane_), n(0), it(-1), valid(true) {
-    step(p);
-  }
-  // to the next block; valid: there is one
-  __device__ __forceinline__ void step(const CacheAttnParams& p) {
-    ++it;
-    while (it >= n) {
-      Segment g;
-      valid = walk.next(p, &g);
+// The block that a wave loads next.
+template <int BT>
+struct Ahead {
+  static constexpr int GPB = BT / 16;  // groups of 16 tokens of a block
+  Walk<BT> walk;
+  Part<BT> part;
+  int it, n;   // block `it` of the part's n
+  int pages;   // of the next 64 groups, one per lane (a dense cache's "page" is the problem)
+  bool valid;  // there is a block
+  __device__ __forceinline__ int token0() const { return part.row.token(part.block0 + it); }
+  __device__ __forceinline__ void start() { valid = true, it = -1, n = 0; }
+  __device__ __forceinline__ void step(const CacheAttnParams& p, int lane) {
+    if (++it >= n) {
+      valid = walk.next(p, &part);
       if (!valid) return;
-      row = g.row, prob = g.prob, c = g.c;
-      first = g.block0 + wave;
-      n = g.block1 > first ? (g.block1 - first + NW - 1) / NW : 0;
       it = 0;
+      n = part.block1 - part.block0;
     }
-    if ((it & 31) != 0) return;
-    pages = prob;
+    if ((it * GPB & 63) != 0) return;
+    pages = part.prob;
     if (!p.cache.table) return;
-    const int t = min(row.token(first + min(it + (lane >> 1), n - 1) * NW) + (lane & 1) * 16, row.len - 1);
-    const int page = p.cache.table[(int64_t)prob * p.cache.pitch + (t >> p.cache.shift)];
+    const int t = min(part.row.token(part.block0 + min(it + lane / GPB, n - 1)) + lane % GPB * 16, part.row.len - 1);
+    const int page = p.cache.table[(int64_t)part.prob * p.cache.pitch + (t >> p.cache.shift)];
     pages = page < 0 ? 0 : page >= p.cache.n_blocks ? p.cache.n_blocks - 1 : page;
   }
-  // Tokens behind the row are its last one again.
-  __device__ __forceinline__ void load(const CacheAttnParams& p, const char* base, int64_t s_block, int64_t s_head, int64_t s_token, uint4 (&dst)[NLOAD]) const {
-    const int t0 = row.token(first + it * NW), in_block = (int)((1u << p.cache.shift) - 1u);
-    base += c * s_head;
-#pragma unroll
-    for (int i = 0; i < NLOAD; ++i) {
-      const char* b = base + (int64_t)__builtin_amdgcn_readlane(pages, (it * 2 + i * TPL / 16) & 63) * s_block;
-      const int t = min(t0 + i * TPL + lane / CH, row.len - 1) & in_block;
-      dst[i] = ld16_stream(b + t * s_token + lane % CH * 16);
-    }
+  // Address of the block's token base + of_lane in K or V; behind the row that of its last token.
+  __device__ __forceinline__ const char* address(const CacheAttnParams& p, const char* cache, int64_t s_block, int64_t s_head, int64_t s_token, int base,
+                                                 int of_lane) const {
+    const int in_block = (int)((1u << p.cache.shift) - 1u), page = __builtin_amdgcn_readlane(pages, (it * GPB + base / 16) & 63);
+    const int t = min(token0() + base + of_lane, part.row.len - 1) & in_block;
+    return cache + part.c * s_head + (int64_t)page * s_block + t * s_token;
   }
-  __device__ __forceinline__ void load_k(const CacheAttnParams& p, uint4 (&dst)[NLOAD]) const {
-    load(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, dst);
+  __device__ __forceinline__ const char* key(const CacheAttnParams& p, int base, int of_lane) const {
+    return address(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, base, of_lane);
   }
-  __device__ __forceinline__ void load_v(const CacheAttnParams& p, uint4 (&dst)[NLOAD]) const {
-    load(p, p.cache.V, p.cache.vs_block, p.cache.vs_head, p.cache.vs_token, dst);
+  __device__ __forceinline__ const char* value(const CacheAttnParams& p, int base, int of_lane) const {
+    return address(p, p.cache.V, p.cache.vs_block, p.cache.vs_head, p.cache.vs_token, base, of_lane);
   }
 };
 
+// ---- what becomes of a part ----------------------------------------------------------------------
+// In LDS a part is its accumulators [heads][D] and (max, sum) per head, not normalised.
+__device__ __forceinline__ int64_t part_at(const CacheAttnParams& p, int group, bool begins) { return ((int64_t)group * 2 + begins) * p.G; }
+
+// A row that a wave has for itself.
+template <int BT, int D>
+__device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part<BT>& g, int lane, const float* acc, const float2* ml) {
+  const int row = g.prob * p.Hkv + g.c;
+  const int64_t head0 = (int64_t)row * p.G + p.g0;
+  for (int i = lane; i < p.gb * (D / 4); i += 64) {
+    const float l = ml[i / (D / 4)].y;
+    const float4 a = reinterpret_cast<const float4*>(acc)[i];
+    reinterpret_cast<float4*>(p.out + head0 * D)[i] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x / l, a.y / l, a.z / l, a.w / l);
+  }
+  if (p.lse && lane < p.gb) p.lse[head0 + lane] = ml[lane].y == 0.f ? -INFINITY : fmaf(ml[lane].x, p.join_scale, logf(ml[lane].y));
+  if (p.by_row && lane == 0) p.joins[row].first = -1;
+}
+
+// A part that a wave leaves in LDS: the first one of its share, or its last one.  row < 0: there is none.
+struct Left {
+  int row, block0, block1, n, row_end;  // as in Part
+};
+template <int BT>
+__device__ __forceinline__ Left left_of(const CacheAttnParams& p, const Part<BT>& g) {
+  return {g.prob * p.Hkv + g.c, g.block0, g.block1, g.row.n, g.row_end};
+}
+
+// The end of a workgroup, behind a barrier: its waves' parts, in order, those of a row merged.  acc(k), ml(k): part k, 2 w the
+// first one of wave w, 2 w + 1 its last one.
+template <int D, typename Acc, typename Ml>
+__device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Shares& shares, const Left (&left)[2 * NW], Acc acc, Ml ml) {
+  const int group = blockIdx.x, tid = threadIdx.x;
+  const float cexp = p.join_scale * 1.44269502162933349609375f;
+  for (int k0 = 0; k0 < 2 * NW;) {
+    const Left first = left[k0];
+    if (first.row < 0) {
+      ++k0;
+      continue;
+    }
+    unsigned set = 1u << k0;
+    int end = first.block1;
+    for (++k0; k0 < 2 * NW; ++k0) {
+      if (left[k0].row < 0) continue;
+      if (left[k0].row != first.row) break;
+      set |= 1u << k0;
+      end = left[k0].block1;
+    }
+    const bool begins = first.block0 == 0, whole = begins && end == first.n;
+    const int64_t head0 = (int64_t)first.row * p.G + p.g0, part0 = part_at(p, group, begins) + p.g0;
+    for (int i = tid; i < p.gb * D; i += NW * 64) {
+      const int h = i / D;
+      float M = -INFINITY;
+      for (unsigned m = set; m; m &= m - 1) M = fmaxf(M, ml(__ffs(m) - 1)[h].x);
+      float a = 0.f, l = 0.f;
+      for (unsigned m = set; m; m &= m - 1) {
+        const int k = __ffs(m) - 1;
+        const float2 v = ml(k)[h];
+        const float f = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * cexp);
+        a += v.x == -INFINITY ? 0.f : acc(k)[i] * f;
+        l += v.y * f;
+      }
+      if (whole) {
+        p.out[head0 * D + i] = l == 0.f ? 0.f : a / l;
+        if (p.lse && i % D == 0) p.lse[head0 + h] = l == 0.f ? -INFINITY : fmaf(M, p.join_scale, logf(l));
+      } else {
+        p.part_acc[part0 * D + i] = a;
+        if (i % D == 0) p.part_ml[part0 + h] = make_float2(M, l);
+      }
+    }
+    // Where a row's parts lie is said by the workgroup that begins it: a record per row (of rows without tokens by clear_empty), or, where there are
+    // more rows than workgroups, one per workgroup.
+    if (tid == 0 && begins && (!whole || p.by_row)) {
+      JoinRecord r = {first.row, -1, 0};
+      if (!whole) {
+        r.first = group;
+        r.last = shares.of(first.row_end - 1) / NW;
+      }
+      p.joins[p.by_row ? first.row : group] = r;
+    }
+  }
+}
+
 // Merges the parts of a row that were left in scratch: a workgroup per (record, head).
-__global__ __launch_bounds__(128) void join_kernel(CacheAttnParams p) {
+template <int D>
+__global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
+  constexpr int C4 = D / 4, Q = 256 / C4, U = 8;  // lanes per part (16 bytes each), parts at a time, rounds in flight at the start
+  __shared__ float factor[kAttnWaves / NW];
+  __shared__ float4 sums[Q][C4];
+  __shared__ float s_max[4];
+  __shared__ double s_den[4];
   const JoinRecord r = p.joins[blockIdx.x];
   if (r.first < 0) return;
-  const int g = blockIdx.y, j = threadIdx.x, sl = threadIdx.x & 31;
-  if (j >= p.D) return;  // wave-uniform
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = blockIdx.y, q = tid / C4, j = tid % C4;
   const int n = r.last - r.first + 1;
-  auto part = [&](int s) { return ((int64_t)(r.first + s) * 2 + (s == 0)) * p.G + g; };
-  float M = -INFINITY, num = 0.f;
-  double den = 0.0;
+  auto part = [&](int s) { return part_at(p, r.first + s, s == 0) + g; };
+  auto acc = [&](int s) { return reinterpret_cast<const float4*>(p.part_acc)[part(s) * C4 + j]; };
+  float4 early[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) early[u] = acc(min(q + u * Q, n - 1));
+  // the parts' factors; one without weight (all of its logits -infinity) is left out
   const float c = p.join_scale * 1.44269502162933349609375f;
-  for (int s0 = 0; s0 < n; s0 += 32) {
-    float2 v = make_float2(-INFINITY, 0.f);
-    if (s0 + sl < n) v = p.part_ml[part(s0 + sl)];
-    float av[32];
-#pragma unroll
-    for (int u = 0; u < 32; ++u) av[u] = s0 + u < n ? p.part_acc[part(s0 + u) * p.D + j] : 0.f;
-    const float Mn = fmaxf(M, swap16_max(row_combine<true, 1>(v.x)));  // both halves of the wave hold the same 32 parts
-    if (Mn == -INFINITY) continue;
-    const float f = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - Mn) * c);
-    const float f0 = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((M - Mn) * c);
-    den = den * f0 + group_sum_f64<32>((double)v.y * f);
-    num *= f0;
-#pragma unroll
-    for (int u = 0; u < 32; ++u)
-      num = fmaf(av[u], __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), u)), num);
-    M = Mn;
+  float M = -INFINITY;
+  for (int s = tid; s < n; s += 256) M = fmaxf(M, p.part_ml[part(s)].x);
+  M = wave_combine<true, 1>(M);
+  if (lane == 0) s_max[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  double den = 0.0;
+  for (int s = tid; s < n; s += 256) {
+    const float2 v = p.part_ml[part(s)];
+    const float f = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * c);
+    factor[s] = v.x == -INFINITY ? -1.f : f;
+    den += (double)v.y * f;
   }
+  den = group_sum_f64<64>(den);
+  if (lane == 0) s_den[wave] = den;
+  __syncthreads();
+  den = (s_den[0] + s_den[1]) + (s_den[2] + s_den[3]);
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& v, float f) {
+    if (f < 0.f) return;
+    a.x = fmaf(v.x, f, a.x), a.y = fmaf(v.y, f, a.y), a.z = fmaf(v.z, f, a.z), a.w = fmaf(v.w, f, a.w);
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (q + u * Q < n) add(early[u], factor[q + u * Q]);
+  for (int s0 = q + U * Q; s0 < n; s0 += 4 * Q) {
+    float4 v[4];
+    float f[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f[u] = s0 + u * Q < n ? factor[s0 + u * Q] : -1.f;
+      if (f[u] >= 0.f) v[u] = acc(s0 + u * Q);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) add(v[u], f[u]);
+  }
+  sums[q][j] = a;
+  __syncthreads();
+  if (tid >= D) return;
+  float num = 0.f;
+#pragma unroll
+  for (int i = 0; i < Q; ++i) num += reinterpret_cast<const float*>(&sums[i][0])[tid];
   const int64_t head = (int64_t)r.row * p.G + g;
-  p.out[head * p.D + j] = den == 0.0 ? 0.f : num / (float)den;
-  if (p.lse && j == 0) p.lse[head] = den == 0.0 ? -INFINITY : fmaf(M, p.join_scale, logf((float)den));
+  p.out[head * D + tid] = den == 0.0 ? 0.f : num / (float)den;
+  if (p.lse && tid == 0) p.lse[head] = den == 0.0 ? -INFINITY : fmaf(M, p.join_scale, logf((float)den));
 }
 
 // bf16 caches.  A wave takes 32 tokens at a time: K goes through the wave's staging buffer in LDS (16-byte chunks, XOR-swizzled) into
@@ -265,7 +372,7 @@ __global__ __launch_bounds__(128) void join_kernel(CacheAttnParams p) {
 // own error is 1e-6, and the matrix cores have nothing else to do: four blocks of 128 dims are 64 KB, 2.5 us of HBM time for a CU.)
 template <int D, int GPAD>
 __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
-  constexpr int BT = 32, NW = 4;
+  constexpr int BT = 32;
   constexpr int CH = D / 8, TPL = 64 / CH, NLOAD = BT / TPL, KSTEPS = D / 32, ROWB = D * 2;
   constexpr int TILES = 16 / GPAD, NT = BT / 16;     // tiles of 16 tokens a q.K accumulator has slots for, tiles of a block
   constexpr int NACC = NT > TILES ? NT / TILES : 1;  // q.K accumulators of a block
@@ -274,20 +381,20 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
   static_assert(GPAD * D * 4 <= BT * ROWB, "a wave's accumulators fit its staging buffer");
   __shared__ uint4 kbuf[NW][BT * CH];
   __shared__ __attribute__((aligned(16))) unsigned short pT[NW][NSET * 16][BT];  // parts of the weights, [part, head][token]
-  __shared__ float2 s_ml[NW][GPAD];
+  __shared__ __attribute__((aligned(16))) float s_first[NW][GPAD * D];  // accumulators of the waves' first parts
+  __shared__ float2 s_ml[2 * NW][GPAD];
+  __shared__ Left s_left[2 * NW];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tq = lane / CH, cl = lane % CH;  // load role: token of a load, 16-byte chunk
   const int n = lane & 15, j = lane >> 4;    // MFMA role: column, row block / k-group
-  const int group = blockIdx.x, g0 = p.g0, gb = p.gb;
-  if (g0 == 0) clear_empty(p);
-  if (tid == 0 && !p.by_row) p.joins[group].first = -1;
-  Walk walk;
-  Shares shares(0, 1);
-  find_share(p, group, lane, &walk, &shares);
-  BlockLoads<D, NW> ahead(p, walk, wave, lane);
-  Segment seg;
-  if (!walk.next(p, &seg)) return;
+  const int number = blockIdx.x * NW + wave, g0 = p.g0, gb = p.gb;
+  if (tid == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
+  if (lane < 2) s_left[2 * wave + lane].row = -1;
+  Ahead<BT> ahead;
+  const Shares shares = ahead.walk.start(p, number, lane);
+  ahead.start();
+  ahead.step(p, lane);
 
   uint4* buf = kbuf[wave];
 #pragma unroll
@@ -305,144 +412,154 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
       if (n % GPAD < gb) qa[kc] = ld16(qrow + 64 * kc);
     }
   };
-  load_q(seg.prob, seg.c);
-  if (ahead.valid) {
-    ahead.load_k(p, kv);
-    ahead.load_v(p, vv);
-  }
-  for (;;) {
-    const Mask mask(p, seg.row.len);
-    const int first = seg.block0 + wave, nblk = seg.block1 > first ? (seg.block1 - first + NW - 1) / NW : 0;
-
-    float m_run[4], l_part[4];
+  auto load_k = [&] {
+#pragma unroll
+    for (int i = 0; i < NLOAD; ++i) kv[i] = ld16_stream(ahead.key(p, i * TPL, tq) + cl * 16);
+  };
+  auto load_v = [&] {
+#pragma unroll
+    for (int i = 0; i < NLOAD; ++i) vv[i] = ld16_stream(ahead.value(p, i * TPL, tq) + cl * 16);
+  };
+  float m_run[4], l_part[4];
+  f32x4_t acc[NDT];
+  auto reset = [&] {
 #pragma unroll
     for (int r = 0; r < 4; ++r) m_run[r] = -INFINITY, l_part[r] = 0.f;
-    f32x4_t acc[NDT];
 #pragma unroll
     for (int nd = 0; nd < NDT; ++nd) acc[nd] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  };
+  if (ahead.valid) {
+    load_q(ahead.part.prob, ahead.part.c);
+    load_k();
+    load_v();
+    reset();
+  }
+  while (ahead.valid) {
+    const Part<BT> part = ahead.part;
+    const int t0 = ahead.token0();
+    const Mask mask(p, part.row.len);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of the buffer are done
+#pragma unroll
+    for (int i = 0; i < NLOAD; ++i) {
+      const int t = i * TPL + tq;
+      buf[t * CH + (cl ^ (t & (CH - 1)))] = kv[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const bool cut = mask.cuts(t0, BT);  // wave-uniform: some of the block's tokens are not attended
+    if (cut) {  // V of those is not to be looked at
+#pragma unroll
+      for (int i = 0; i < NLOAD; ++i)
+        if (!mask.at(t0 + i * TPL + tq)) vv[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    ahead.step(p, lane);  // (V of the present block is on its way already)
+    const bool last = !ahead.valid || ahead.it == 0;  // the part's last block
+    if (ahead.valid) load_k();
 
-    for (int it = 0; it < nblk; ++it) {
-      const int t0 = seg.row.token(first + it * NW);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of the buffer are done
+    float x[NACC][4];
 #pragma unroll
-      for (int i = 0; i < NLOAD; ++i) {
-        const int t = i * TPL + tq;
-        buf[t * CH + (cl ^ (t & (CH - 1)))] = kv[i];
+    for (int ts = 0; ts < NT; ++ts) {
+      const int t = ts * 16 + n;
+      f32x4_t d = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kc = 0; kc < KSTEPS; ++kc) {
+        const uint4 bb = buf[t * CH + ((4 * kc + j) ^ (n & (CH - 1)))];
+        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, qa[kc]), __builtin_bit_cast(bf16x8_t, bb), d, 0, 0, 0);
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      const bool cut = mask.cuts(t0, BT);  // wave-uniform: some of the block's tokens are not attended
-      if (cut) {  // V of those is not to be looked at
 #pragma unroll
-        for (int i = 0; i < NLOAD; ++i)
-          if (!mask.at(t0 + i * TPL + tq)) vv[i] = make_uint4(0u, 0u, 0u, 0u);
-      }
-      ahead.step(p);  // (V of the present block is on its way already)
-      if (ahead.valid) ahead.load_k(p, kv);
-
-      float x[NACC][4];
+      for (int r = 0; r < 4; ++r) x[ts / TILES][r] = ts % TILES == 0 || tslot == ts % TILES ? d[r] : x[ts / TILES][r];
+    }
+    if (last && ahead.valid) load_q(ahead.part.prob, ahead.part.c);
 #pragma unroll
-      for (int ts = 0; ts < NT; ++ts) {
-        const int t = ts * 16 + n;
-        f32x4_t d = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int a = 0; a < NACC; ++a) {
+      const int tile = a * TILES + tslot;
+      const bool in = tile < NT && (!cut || mask.at(t0 + tile * 16 + n));
 #pragma unroll
-        for (int kc = 0; kc < KSTEPS; ++kc) {
-          const uint4 bb = buf[t * CH + ((4 * kc + j) ^ (n & (CH - 1)))];
-          d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, qa[kc]), __builtin_bit_cast(bf16x8_t, bb), d, 0, 0, 0);
-        }
+      for (int r = 0; r < 4; ++r) x[a][r] = in && hbase + r < gb ? x[a][r] : -INFINITY;
+    }
+    // online softmax, once per (token, head), in units of the products; lanes with the same heads agree on the maximum
+    float corr[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x[ts / TILES][r] = ts % TILES == 0 || tslot == ts % TILES ? d[r] : x[ts / TILES][r];
-      }
+    for (int r = 0; r < 4; ++r) {
+      float bm = x[0][r];
+#pragma unroll
+      for (int a = 1; a < NACC; ++a) bm = fmaxf(bm, x[a][r]);
+      bm = group16_max(bm);
+      if (GPAD <= 4) bm = swap16_max(bm);
+      if (GPAD <= 8) bm = swap32_max(bm);
+      const float mn = fmaxf(m_run[r], bm);
+      corr[r] = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[r] - mn) * cexp);
+      float lsum = 0.f;
 #pragma unroll
       for (int a = 0; a < NACC; ++a) {
+        const float w = x[a][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[a][r] - mn) * cexp);
+        lsum += w;
         const int tile = a * TILES + tslot;
-        const bool in = tile < NT && (!cut || mask.at(t0 + tile * 16 + n));
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[a][r] = in && hbase + r < gb ? x[a][r] : -INFINITY;
-      }
-      // online softmax, once per (token, head), in units of the products; lanes with the same heads agree on the maximum
-      float corr[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float bm = x[0][r];
-#pragma unroll
-        for (int a = 1; a < NACC; ++a) bm = fmaxf(bm, x[a][r]);
-        bm = group16_max(bm);
-        if (GPAD <= 4) bm = swap16_max(bm);
-        if (GPAD <= 8) bm = swap32_max(bm);
-        const float mn = fmaxf(m_run[r], bm);
-        corr[r] = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[r] - mn) * cexp);
-        float lsum = 0.f;
-#pragma unroll
-        for (int a = 0; a < NACC; ++a) {
-          const float w = x[a][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[a][r] - mn) * cexp);
-          lsum += w;
-          const int tile = a * TILES + tslot;
-          if (tile < NT) {
-            // three parts of 8 bits; one that is 0 beside a weight that is not becomes bf16's smallest number, so that an infinite value's product
-            // with it is no NaN
-            const uint32_t hi = __float_as_uint(w) & 0xFFFF0000u;
-            const float rest = w - __uint_as_float(hi);
-            uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
-            uint32_t lo = __float_as_uint(rest - __uint_as_float(mid));
-            if (hi != 0u) {
-              mid = mid == 0u ? 0x10000u : mid;
-              lo = (lo >> 16) == 0u ? 0x10000u : lo;
-            }
-            const int col = tile * 16 + n;
-            pT[wave][hbase + r][col] = (unsigned short)(hi >> 16);
-            pT[wave][GPAD + hbase + r][col] = (unsigned short)(mid >> 16);
-            pT[wave][2 * GPAD + hbase + r][col] = (unsigned short)(lo >> 16);
-            if (GPAD == 8) pT[wave][3 * GPAD + hbase + r][col] = hi != 0u;  // beside the lows: no 0 there either
+        if (tile < NT) {
+          // three parts of 8 bits; one that is 0 beside a weight that is not becomes bf16's smallest number, so that an infinite value's product
+          // with it is no NaN
+          const uint32_t hi = __float_as_uint(w) & 0xFFFF0000u;
+          const float rest = w - __uint_as_float(hi);
+          uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
+          uint32_t lo = __float_as_uint(rest - __uint_as_float(mid));
+          if (hi != 0u) {
+            mid = mid == 0u ? 0x10000u : mid;
+            lo = (lo >> 16) == 0u ? 0x10000u : lo;
           }
+          const int col = tile * 16 + n;
+          pT[wave][hbase + r][col] = (unsigned short)(hi >> 16);
+          pT[wave][GPAD + hbase + r][col] = (unsigned short)(mid >> 16);
+          pT[wave][2 * GPAD + hbase + r][col] = (unsigned short)(lo >> 16);
+          if (GPAD == 8) pT[wave][3 * GPAD + hbase + r][col] = hi != 0u;  // beside the lows: no 0 there either
         }
-        l_part[r] = l_part[r] * corr[r] + lsum;
-        m_run[r] = mn;
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // weights visible; q.K's reads of the buffer done
+      l_part[r] = l_part[r] * corr[r] + lsum;
+      m_run[r] = mn;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // weights visible; q.K's reads of the buffer done
 #pragma unroll
-      for (int i = 0; i < NLOAD; ++i) {
-        const int t = i * TPL + tq;
-        buf[t * CH + (cl ^ vswz(t))] = vv[i];
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if (ahead.valid) ahead.load_v(p, vv);
+    for (int i = 0; i < NLOAD; ++i) {
+      const int t = i * TPL + tq;
+      buf[t * CH + (cl ^ vswz(t))] = vv[i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (ahead.valid) load_v();
 
-      uint4 pa[NSET];
+    uint4 pa[NSET];
 #pragma unroll
-      for (int i = 0; i < NSET; ++i) pa[i] = *reinterpret_cast<const uint4*>(&pT[wave][16 * i + n][8 * j]);
+    for (int i = 0; i < NSET; ++i) pa[i] = *reinterpret_cast<const uint4*>(&pT[wave][16 * i + n][8 * j]);
 #pragma unroll
-      for (int nd = 0; nd < NDT; ++nd) {
+    for (int nd = 0; nd < NDT; ++nd) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[nd][r] *= corr[r];  // row 4j + r belongs to head hbase + r whatever part it is
-        // transposed read: lane s of 16 gives the address of 4 dims of token s / 4 and receives its own dim of 4 tokens
-        typedef short v4s_t __attribute__((ext_vector_type(4)));
-        const int tu = 8 * j + (n >> 2);
-        const int cch = (2 * nd + ((n & 3) >> 1)) ^ vswz(tu);  // vswz(tu) = vswz(tu + 4)
-        const unsigned short* b16 = reinterpret_cast<const unsigned short*>(buf);
-        const v4s_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s_t*)(b16 + (tu * CH + cch) * 8 + (n & 1) * 4));
-        const v4s_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s_t*)(b16 + ((tu + 4) * CH + cch) * 8 + (n & 1) * 4));
-        struct { v4s_t a, b; } pair = {x0, x1};
-        const uint4 vb = __builtin_bit_cast(uint4, pair);
+      for (int r = 0; r < 4; ++r) acc[nd][r] *= corr[r];  // row 4j + r belongs to head hbase + r whatever part it is
+      // transposed read: lane s of 16 gives the address of 4 dims of token s / 4 and receives its own dim of 4 tokens
+      typedef short v4s_t __attribute__((ext_vector_type(4)));
+      const int tu = 8 * j + (n >> 2);
+      const int cch = (2 * nd + ((n & 3) >> 1)) ^ vswz(tu);  // vswz(tu) = vswz(tu + 4)
+      const unsigned short* b16 = reinterpret_cast<const unsigned short*>(buf);
+      const v4s_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) v4s_t*)(b16 + (tu * CH + cch) * 8 + (n & 1) * 4));
+      const v4s_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) v4s_t*)(b16 + ((tu + 4) * CH + cch) * 8 + (n & 1) * 4));
+      struct { v4s_t a, b; } pair = {x0, x1};
+      const uint4 vb = __builtin_bit_cast(uint4, pair);
 #pragma unroll
-        for (int i = 0; i < NSET; ++i)
-          acc[nd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pa[i]), __builtin_bit_cast(bf16x8_t, vb), acc[nd], 0, 0, 0);
-      }
+      for (int i = 0; i < NSET; ++i)
+        acc[nd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pa[i]), __builtin_bit_cast(bf16x8_t, vb), acc[nd], 0, 0, 0);
     }
 
-    Segment next;
-    const bool more = walk.next(p, &next);
-    if (more) load_q(next.prob, next.c);
-    // the wave's totals: weights over the lanes that share a head, accumulators over the rows that hold its parts
+    if (!last) continue;
+    // the part's totals: weights over the lanes that share a head, accumulators over the rows that hold its parts
+    const bool whole = part.block0 == 0 && part.block1 == part.row.n, first = !whole && ahead.valid;
+    const int k = 2 * wave + !first;
+    if (!whole && lane == 0) s_left[k] = left_of(p, part);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float ls = group_sum<16>(l_part[r]);
       if (GPAD <= 4) ls = swap16_sum(ls);
       if (GPAD <= 8) ls = swap32_sum(ls);
-      if (n == 0 && j < GPAD / 4) s_ml[wave][hbase + r] = make_float2(m_run[r], ls);
+      if (n == 0 && j < GPAD / 4) s_ml[k][hbase + r] = make_float2(m_run[r], ls);
     }
-    float* s_acc = reinterpret_cast<float*>(buf);  // [GPAD][D]
+    float* s_acc = first ? s_first[wave] : reinterpret_cast<float*>(buf);  // [GPAD][D]
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int nd = 0; nd < NDT; ++nd)
@@ -456,41 +573,14 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
         if (GPAD <= 8) a = swap32_sum(a);
         if (4 * j < GPAD) s_acc[(4 * j + r) * D + nd * 16 + n] = a;
       }
-    __syncthreads();
-    constexpr int kAccStride = BT * ROWB / 4;  // floats between the waves' buffers
-    const float* all = reinterpret_cast<const float*>(&kbuf[0][0]);
-    const int64_t part = ((int64_t)group * 2 + (seg.block0 == 0)) * p.G + g0, head0 = ((int64_t)seg.prob * p.Hkv + seg.c) * p.G + g0;
-#pragma unroll
-    for (int i0 = 0; i0 < GPAD * D; i0 += NW * 64) {
-      const int g = (i0 + tid) / D, jj = tid % D;
-      if (g >= gb) break;
-      float2 ml[NW];
-      float M = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        ml[w] = s_ml[w][g];
-        M = fmaxf(M, ml[w].x);
-      }
-      float a = 0.f, ls = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float f = ml[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[w].x - M) * cexp);
-        a += ml[w].x == -INFINITY ? 0.f : all[w * kAccStride + g * D + jj] * f;
-        ls += ml[w].y * f;
-      }
-      if (seg.whole()) {
-        p.out[(head0 + g) * D + jj] = ls == 0.f ? 0.f : a / ls;
-        if (p.lse && jj == 0) p.lse[head0 + g] = ls == 0.f ? -INFINITY : fmaf(M, p.scale, logf(ls));
-      } else {
-        p.part_acc[(part + g) * D + jj] = a;
-        if (jj == 0) p.part_ml[part + g] = make_float2(M, ls);
-      }
-    }
-    if (tid == 0) leave_record(p, shares, seg, group);
-    if (!more) return;
-    __syncthreads();  // buffers and s_ml are free again
-    seg = next;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (whole) write_row<BT, D>(p, part, lane, s_acc, s_ml[k]);
+    reset();
   }
+  __syncthreads();
+  finish_group<D>(p, shares, s_left, [&](int k) { return k & 1 ? reinterpret_cast<const float*>(kbuf[k >> 1]) : s_first[k >> 1]; },
+                  [&](int k) { return s_ml[k]; });
+  if (g0 == 0) clear_empty(p);
 }
 
 // fp32 caches.  Both products and the sums in fp64 (an fp32 logit of magnitude 100 would be off by 2.5e-5, and so would its softmax weight);
@@ -498,182 +588,176 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
 // heads and lanes change places, and lane s of the eight ends with head s's logit, whose weight it computes once and leaves in LDS for the lanes that
 // hold V's chunks.  GB heads, at most 8.
 template <int D, int GB>
-__global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(CacheAttnParams p) {
-  constexpr int NW = D == 128 ? 8 : 4, BT = kBlock * kGroupBlocks / NW, kThreads = NW * 64;
-  constexpr int CH = D / 4, GPB = BT / 16;
+__global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(CacheAttnParams p) {
+  constexpr int BT = D == 128 ? 16 : 32;
+  constexpr int CH = D / 4;
   constexpr bool LATE_V = GB >= 4;             // V's block after the logits, not with K's: else registers spill
   constexpr int NG = BT / 8, NC = CH / 8;      // K: groups of 8 tokens, a lane's chunks of a token
   constexpr int TPL = 64 / CH, NV = BT / TPL;  // V: tokens per load, loads
   constexpr int GP = (GB + 1) / 2 * 2;         // weights of a token in LDS: whole 16-byte pairs
-  __shared__ __attribute__((aligned(16))) double qd[GB * D];
+  __shared__ __attribute__((aligned(16))) double s_q[NW][GB * D];
   __shared__ __attribute__((aligned(16))) double pw[NW][BT][GP];
-  __shared__ float s_acc[NW][GB][D];
-  __shared__ float s_m[NW][GB];
-  __shared__ double s_l[NW][GB];
+  __shared__ __attribute__((aligned(16))) float s_acc[2 * NW][GB * D];
+  __shared__ float2 s_ml[2 * NW][GB];
+  __shared__ Left s_left[2 * NW];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int t8 = lane >> 3, sl = lane & 7;   // K role: token of a group, share of a token; head, once the logits are summed
   const int tq = lane / CH, cl = lane % CH;  // V role: token of a load, chunk
-  const int group = blockIdx.x, g0 = p.g0;
-  if (g0 == 0) clear_empty(p);
-  if (tid == 0 && !p.by_row) p.joins[group].first = -1;
-  Walk walk;
-  Shares shares(0, 1);
-  find_share(p, group, lane, &walk, &shares);
+  const int number = blockIdx.x * NW + wave, g0 = p.g0;
+  if (tid == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
+  if (lane < 2) s_left[2 * wave + lane].row = -1;
+  Ahead<BT> ahead;
+  const Shares shares = ahead.walk.start(p, number, lane);
+  ahead.start();
+  ahead.step(p, lane);
 
-  for (Segment seg; walk.next(p, &seg);) {
-    const RowBlocks row = seg.row;
-    const int prob = seg.prob, c = seg.c;
-    const Mask mask(p, row.len);
-    const int64_t head0 = ((int64_t)prob * p.Hkv + c) * p.G + g0;
-    // 128 dims: two waves share a block
-    constexpr int SHARE = kBlock / BT;
-    auto token0 = [&](int it) { return row.token(seg.block0 + wave / SHARE + it * kGroupBlocks) + wave % SHARE * BT; };
-    int nblk = (seg.block1 - seg.block0 - wave / SHARE + kGroupBlocks - 1) / kGroupBlocks;
-    if (nblk > 0 && token0(nblk - 1) >= row.len) --nblk;
-
-    const char* Kb = p.cache.K + c * p.cache.ks_head;
-    const char* Vb = p.cache.V + c * p.cache.vs_head;
-    const int32_t* tab = p.cache.table ? p.cache.table + (int64_t)prob * p.cache.pitch : nullptr;
-    const int in_block = (int)((1u << p.cache.shift) - 1u);
-    int my_block = prob;  // paged: pages of the wave's next 64 groups of 16 tokens, one per lane
-    auto fill = [&](int it0) {
-      if (!tab) return;
-      const int it = min(it0 + lane / GPB, nblk - 1);
-      const int t = min(token0(it) + lane % GPB * 16, row.len - 1);
-      const int b = tab[t >> p.cache.shift];
-      my_block = b < 0 ? 0 : b >= p.cache.n_blocks ? p.cache.n_blocks - 1 : b;
-    };
-    // token `base + of_lane` of block it, behind the row its last one
-    auto address = [&](const char* at, int64_t s_block, int64_t s_token, int it, int base, int of_lane) {
-      const int t = min(token0(it) + base + of_lane, row.len - 1);
-      return at + (int64_t)__builtin_amdgcn_readlane(my_block, (it * GPB + base / 16) & 63) * s_block + (t & in_block) * s_token;
-    };
-    uint4 kv[NG][NC], vv[NV];
-    auto load_k = [&](int it) {
+  double* qd = s_q[wave];
+  uint4 kv[NG][NC], vv[NV];
+  auto load_k = [&] {
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const char* a = address(Kb, p.cache.ks_block, p.cache.ks_token, it, 8 * g, t8) + sl * 16;
+    for (int g = 0; g < NG; ++g) {
+      const char* a = ahead.key(p, 8 * g, t8) + sl * 16;
 #pragma unroll
-        for (int ch = 0; ch < NC; ++ch) kv[g][ch] = ld16(a + ch * 128);
-      }
-    };
-    auto load_v = [&](int it) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) vv[i] = ld16(address(Vb, p.cache.vs_block, p.cache.vs_token, it, i * TPL, tq) + cl * 16);
-    };
-    if (nblk > 0) {
-      fill(0);
-      load_k(0);
-      if (!LATE_V) load_v(0);
+      for (int ch = 0; ch < NC; ++ch) kv[g][ch] = ld16(a + ch * 128);
     }
-    for (int i = tid; i < GB * D; i += kThreads) qd[i] = (double)((const float*)p.q)[head0 * D + i];
-    __syncthreads();
-
-    float m = -INFINITY;  // of head sl
-    double l = 0.0, acc[GB][4];
+  };
+  auto load_v = [&] {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) vv[i] = ld16(ahead.value(p, i * TPL, tq) + cl * 16);
+  };
+  constexpr int NQ = (GB * D + 63) / 64;
+  float qv[NQ];  // the next part's queries
+  auto load_q = [&](int prob, int c) {
+    const float* q = (const float*)p.q + (((int64_t)prob * p.Hkv + c) * p.G + g0) * D;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) qv[i] = q[i * 64 + lane];
+  };
+  auto keep_q = [&] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) qd[i * 64 + lane] = (double)qv[i];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
+  float m = -INFINITY;  // of head sl
+  double l = 0.0, acc[GB][4];
+  auto reset = [&] {
+    m = -INFINITY;
+    l = 0.0;
 #pragma unroll
     for (int g = 0; g < GB; ++g)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[g][e] = 0.0;
-
-    for (int it = 0; it < nblk; ++it) {
-      const int t0 = token0(it);
-      const bool cut = mask.cuts(t0, BT);
-      double x[NG];  // of head sl, token 8 g + t8
+  };
+  if (ahead.valid) {
+    load_q(ahead.part.prob, ahead.part.c);
+    load_k();
+    if (!LATE_V) load_v();
+    reset();
+    keep_q();
+  }
+  while (ahead.valid) {
+    const Part<BT> part = ahead.part;
+    const int t0 = ahead.token0();
+    const Mask mask(p, part.row.len);
+    const bool cut = mask.cuts(t0, BT);
+    double x[NG];  // of head sl, token 8 g + t8
 #pragma unroll
-      for (int gg = 0; gg < NG; gg += 2) {
+    for (int gg = 0; gg < NG; gg += 2) {
 #pragma unroll
-        for (int hh = 0; hh < GB; hh += 4) {
-          asm volatile("" ::: "memory");  // the queries are read again, not held for the other groups
-          double a[2][4];
+      for (int hh = 0; hh < GB; hh += 4) {
+        asm volatile("" ::: "memory");  // the queries are read again, not held for the other groups
+        double a[2][4];
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int h = 0; h < 4; ++h) a[u][h] = 0.0;
+          for (int h = 0; h < 4; ++h) a[u][h] = 0.0;
 #pragma unroll
-          for (int ch = 0; ch < NC; ++ch) {
-            double kd[2][4];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              kd[u][0] = (double)__uint_as_float(kv[gg + u][ch].x);
-              kd[u][1] = (double)__uint_as_float(kv[gg + u][ch].y);
-              kd[u][2] = (double)__uint_as_float(kv[gg + u][ch].z);
-              kd[u][3] = (double)__uint_as_float(kv[gg + u][ch].w);
-            }
-#pragma unroll
-            for (int h = 0; h < 4 && hh + h < GB; ++h) {
-              const double* q = qd + (hh + h) * D + (ch * 8 + sl) * 4;
-#pragma unroll
-              for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) a[u][h] = fma(kd[u][e], q[e], a[u][h]);
-            }
-          }
-          // over the eight lanes of a token; lane s keeps head s
+        for (int ch = 0; ch < NC; ++ch) {
+          double kd[2][4];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const double r = eight_lane_sums<GB>(a[u], sl);
-            x[gg + u] = hh == 0 || sl >= 4 ? r : x[gg + u];
+            kd[u][0] = (double)__uint_as_float(kv[gg + u][ch].x);
+            kd[u][1] = (double)__uint_as_float(kv[gg + u][ch].y);
+            kd[u][2] = (double)__uint_as_float(kv[gg + u][ch].z);
+            kd[u][3] = (double)__uint_as_float(kv[gg + u][ch].w);
+          }
+#pragma unroll
+          for (int h = 0; h < 4 && hh + h < GB; ++h) {
+            const double* q = qd + (hh + h) * D + (ch * 8 + sl) * 4;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) a[u][h] = fma(kd[u][e], q[e], a[u][h]);
           }
         }
-      }
-      if (LATE_V) load_v(it);
-      const bool more = it + 1 < nblk;
-      if (more) {
-        if ((((it + 1) * GPB) & 63) == 0) fill(it + 1);
-        load_k(it + 1);
-      }
-
-      // softmax weights, once per (token, head)
-      float bm = -INFINITY;
+        // over the eight lanes of a token; lane s keeps head s
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const bool in = sl < GB && (!cut || mask.at(t0 + 8 * g + t8));
-        x[g] = in ? x[g] * (1.0 / sqrt((double)D)) : -INFINITY;
-        bm = fmaxf(bm, (float)x[g]);
-      }
-      bm = fmaxf(bm, dpp_f32<0x128>(bm));  // row_ror:8
-      bm = swap32_max(swap16_max(bm));
-      const float mn = fmaxf(m, bm);
-      const float corr = mn == -INFINITY ? 1.f : exp_fast(m - mn);
-      l *= (double)corr;
-      m = mn;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's weights are read
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const float w = x[g] == -INFINITY ? 0.f : exp_fast((float)(x[g] - (double)mn));
-        l += (double)w;
-        if (sl < GB) pw[wave][8 * g + t8][sl] = (double)w;
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-
-      if (cut) {  // what is not attended is not to be looked at
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (!mask.at(t0 + i * TPL + tq)) vv[i] = make_uint4(0u, 0u, 0u, 0u);
-      }
-#pragma unroll
-      for (int g = 0; g < GB; ++g) {
-        const double f = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(corr), g));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[g][e] *= f;
-      }
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const double v[4] = {(double)__uint_as_float(vv[i].x), (double)__uint_as_float(vv[i].y), (double)__uint_as_float(vv[i].z),
-                             (double)__uint_as_float(vv[i].w)};
-#pragma unroll
-        for (int g = 0; g < GB; ++g) {
-          const double w = pw[wave][i * TPL + tq][g];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[g][e] = fma(w, v[e], acc[g][e]);
+        for (int u = 0; u < 2; ++u) {
+          const double r = eight_lane_sums<GB>(a[u], sl);
+          x[gg + u] = hh == 0 || sl >= 4 ? r : x[gg + u];
         }
       }
-      if (!LATE_V && more) load_v(it + 1);
     }
+    if (LATE_V) load_v();
+    ahead.step(p, lane);
+    const bool last = !ahead.valid || ahead.it == 0;  // the part's last block
+    if (ahead.valid) load_k();
 
-    // the wave's totals: over the lanes that share a chunk of V, and those that share a head
+    // softmax weights, once per (token, head)
+    float bm = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const bool in = sl < GB && (!cut || mask.at(t0 + 8 * g + t8));
+      x[g] = in ? x[g] * (1.0 / sqrt((double)D)) : -INFINITY;
+      bm = fmaxf(bm, (float)x[g]);
+    }
+    bm = fmaxf(bm, dpp_f32<0x128>(bm));  // row_ror:8
+    bm = swap32_max(swap16_max(bm));
+    const float mn = fmaxf(m, bm);
+    const float corr = mn == -INFINITY ? 1.f : exp_fast(m - mn);
+    l *= (double)corr;
+    m = mn;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's weights are read
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float w = x[g] == -INFINITY ? 0.f : exp_fast((float)(x[g] - (double)mn));
+      l += (double)w;
+      if (sl < GB) pw[wave][8 * g + t8][sl] = (double)w;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+
+    if (cut) {  // what is not attended is not to be looked at
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (!mask.at(t0 + i * TPL + tq)) vv[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int g = 0; g < GB; ++g) {
+      const double f = (double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(corr), g));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[g][e] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const double v[4] = {(double)__uint_as_float(vv[i].x), (double)__uint_as_float(vv[i].y), (double)__uint_as_float(vv[i].z),
+                           (double)__uint_as_float(vv[i].w)};
+#pragma unroll
+      for (int g = 0; g < GB; ++g) {
+        const double w = pw[wave][i * TPL + tq][g];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[g][e] = fma(w, v[e], acc[g][e]);
+      }
+    }
+    if (!LATE_V && ahead.valid) load_v();
+
+    if (!last) continue;
+    // the part's totals: over the lanes that share a chunk of V, and those that share a head
+    if (ahead.valid) load_q(ahead.part.prob, ahead.part.c);
+    const bool whole = part.block0 == 0 && part.block1 == part.row.n, first = !whole && ahead.valid;
+    const int k = 2 * wave + !first;
+    if (!whole && lane == 0) s_left[k] = left_of(p, part);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int g = 0; g < GB; ++g)
 #pragma unroll
@@ -681,40 +765,20 @@ __global__ __launch_bounds__(D == 128 ? 512 : 256) void cache_attn_f32_kernel(Ca
         double a = acc[g][e];
         if (CH == 16) a += swap16_f64(a);
         a = swap32_sum_f64(a);
-        if (tq == 0) s_acc[wave][g][cl * 4 + e] = (float)a;
+        if (tq == 0) s_acc[k][g * D + cl * 4 + e] = (float)a;
       }
     l += dpp_f64<0x128>(l);
     l += swap16_f64(l);
     l = swap32_sum_f64(l);
-    if (lane < GB) {
-      s_m[wave][lane] = m;
-      s_l[wave][lane] = l;
-    }
-    __syncthreads();
-    const int64_t part = ((int64_t)group * 2 + (seg.block0 == 0)) * p.G + g0;
-    for (int i = tid; i < GB * D; i += kThreads) {
-      const int g = i / D, jj = i % D;
-      float M = s_m[0][g];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w][g]);
-      double a = 0.0, ls = 0.0;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const double f = s_m[w][g] == -INFINITY ? 0.0 : (double)exp_fast(s_m[w][g] - M);
-        a += s_m[w][g] == -INFINITY ? 0.0 : (double)s_acc[w][g][jj] * f;
-        ls += s_l[w][g] * f;
-      }
-      if (seg.whole()) {
-        p.out[(head0 + g) * D + jj] = ls == 0.0 ? 0.f : (float)(a / ls);
-        if (p.lse && jj == 0) p.lse[head0 + g] = ls == 0.0 ? -INFINITY : (float)((double)M + log(ls));
-      } else {
-        p.part_acc[(part + g) * D + jj] = (float)a;
-        if (jj == 0) p.part_ml[part + g] = make_float2(M, (float)ls);
-      }
-    }
-    if (tid == 0) leave_record(p, shares, seg, group);
-    __syncthreads();  // LDS is free again
+    if (lane < GB) s_ml[k][lane] = make_float2(m, (float)l);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (whole) write_row<BT, D>(p, part, lane, s_acc[k], s_ml[k]);
+    reset();
+    if (ahead.valid) keep_q();
   }
+  __syncthreads();
+  finish_group<D>(p, shares, s_left, [&](int k) { return s_acc[k]; }, [&](int k) { return s_ml[k]; });
+  if (g0 == 0) clear_empty(p);
 }
 
 template <int D, int GB = 1>
@@ -722,12 +786,12 @@ void launch_f32(const CacheAttnParams& p, hipStream_t s) {
   if constexpr (GB < 8) {
     if (p.gb > GB) return launch_f32<D, GB + 1>(p, s);
   }
-  hipLaunchKernelGGL((cache_attn_f32_kernel<D, GB>), dim3((unsigned)p.n_groups), dim3(D == 128 ? 512 : 256), 0, s, p);
+  hipLaunchKernelGGL((cache_attn_f32_kernel<D, GB>), dim3((unsigned)((p.n_waves + NW - 1) / NW)), dim3(NW * 64), 0, s, p);
 }
 
 template <int D>
 void launch_bf16(const CacheAttnParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)p.n_groups);
+  const dim3 grid((unsigned)((p.n_waves + NW - 1) / NW));
   if (p.gb <= 4) hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 4>), grid, dim3(256), 0, s, p);
   else if (p.gb <= 8) hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 8>), grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 16>), grid, dim3(256), 0, s, p);
@@ -746,7 +810,9 @@ hipError_t launch_cache_attn(const CacheAttnParams& p, bool join, hipStream_t s)
     if (e != hipSuccess) return e;
   }
   if (!join) return hipSuccess;
-  hipLaunchKernelGGL(join_kernel, dim3((unsigned)(p.by_row ? p.P * p.Hkv : p.n_groups), (unsigned)p.G), dim3(128), 0, s, p);
+  const dim3 grid((unsigned)(p.by_row ? p.P * p.Hkv : (p.n_waves + NW - 1) / NW), (unsigned)p.G);
+  if (p.D == 128) hipLaunchKernelGGL(join_kernel<128>, grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL(join_kernel<64>, grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -33,15 +33,17 @@ struct RotaryParams {
 };
 hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
 
-constexpr int kBlock = 32;         // tokens of a row that a wave takes at a time
-constexpr int kAttnGroups = 512;   // workgroups of an attention launch at most: two per CU
-constexpr int kGroupBlocks = 4;    // blocks a workgroup has work for at a time
-constexpr int kRowWeight = 8;      // a row's beginning and end, in blocks
+constexpr int kAttnGroups = 512;  // workgroups of an attention launch at most: two per CU,
+constexpr int kAttnWaves = 2048;  // of four waves
+constexpr int kRowWeight = 1;     // a row's beginning and end, in blocks
 
 // A row whose parts are to be joined, those of workgroups first (its second slot) and first + 1 .. last (their first slots).
 struct JoinRecord {
   int row, first, last;  // first < 0: nothing to do
 };
+
+// Tokens of a block: 16 KB of K and V are in flight for a wave.
+inline int attn_block(int dtype, int head_dim) { return dtype == 1 && head_dim == 128 ? 16 : 32; }
 
 struct CacheAttnParams {
   FullCache cache;
@@ -50,14 +52,14 @@ struct CacheAttnParams {
   const int32_t* lens;
   int P, Hq, Hkv, G, D, dtype;
   int S, W, max_len;
-  bool whole_rows;  // rows are short and never split
-  bool by_row;      // a join record per row, else one per workgroup
-  int n_groups;     // workgroups
+  int row_parts;  // short rows: each is split into that many parts, whatever its length; else 0
+  bool by_row;    // a join record per row, else one per workgroup
+  int n_waves;
   int g0, gb;    // the group's heads that a launch handles
   float scale;       // 1 / sqrt(head_dim)
   float join_scale;  // the parts' maxima times this are logits: scale where they are products (bf16), 1 where they are logits (fp32)
-  float* part_acc;    // [n_groups][2][G][D]
-  float2* part_ml;    // [n_groups][2][G]
+  float* part_acc;    // [kAttnGroups][2][G][D]
+  float2* part_ml;    // [kAttnGroups][2][G]
   JoinRecord* joins;  // [kAttnGroups]
 };
 hipError_t launch_cache_attn(const CacheAttnParams& p, bool join, hipStream_t s);

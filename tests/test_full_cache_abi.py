@@ -216,7 +216,7 @@ def test_attn_workspace():
     n = fc._fn("sagekvc_attn_workspace_bytes")
     assert n(None) == 0
     desc = sk.CacheDesc(3, 8, 2, 128, sk.BF16, 100, 0, 0, 0, 0, 0, 0)  # strides do not enter
-    assert n(byref(desc)) == 2 * 512 * 4 * (128 * 4 + 8) + 512 * 16
+    assert n(byref(desc)) == 2 * 512 * 4 * (128 * 4 + 8) + 512 * 12
     desc.head_dim = 96
     assert n(byref(desc)) == 0
 
