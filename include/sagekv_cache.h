@@ -8,7 +8,7 @@
  * before anything is launched, calls can be recorded into a HIP graph); their names start with sagekvc_.
  *
  * A full cache is either dense, K[p][c][t][j] at p*stride_problem + c*stride_head + t*stride_token + j (elements), or paged as
- * in sagekv_select_paged: the same head and token strides inside a page, a block table per problem.  Here a problem is
+ * in sagekv_select_paged: the same head and token strides inside a page, a block table per problem; a token's stride is less than 2^24 bytes.  Here a problem is
  * one sequence (or one layer of one), and every problem has its own length.
  */
 #ifndef SAGEKV_CACHE_H

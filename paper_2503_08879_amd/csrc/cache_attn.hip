@@ -156,15 +156,18 @@ struct Walk {
   }
 };
 
-// Problems without tokens: out = 0, lse = -infinity.
-__device__ __forceinline__ void clear_empty(const CacheAttnParams& p) {
-  for (int prob = blockIdx.x; prob < p.P; prob += gridDim.x) {
-    if (length_of(p, prob) > 0) continue;
-    for (int i = threadIdx.x; i < p.Hq * p.D; i += blockDim.x) p.out[(int64_t)prob * p.Hq * p.D + i] = 0.f;
-    if (p.lse)
-      for (int i = threadIdx.x; i < p.Hq; i += blockDim.x) p.lse[(int64_t)prob * p.Hq + i] = -INFINITY;
-    if (p.by_row)
-      for (int c = threadIdx.x; c < p.Hkv; c += blockDim.x) p.joins[prob * p.Hkv + c].first = -1;
+// Problems without tokens: out = 0, lse = -infinity.  length: of the workgroup's first problem, read early.
+__device__ __forceinline__ void clear_empty(const CacheAttnParams& p, int length) {
+  for (int prob = blockIdx.x; prob < p.P;) {
+    if (length <= 0) {
+      for (int i = threadIdx.x; i < p.Hq * p.D; i += blockDim.x) p.out[(int64_t)prob * p.Hq * p.D + i] = 0.f;
+      if (p.lse)
+        for (int i = threadIdx.x; i < p.Hq; i += blockDim.x) p.lse[(int64_t)prob * p.Hq + i] = -INFINITY;
+      if (p.by_row)
+        for (int c = threadIdx.x; c < p.Hkv; c += blockDim.x) p.joins[prob * p.Hkv + c].first = -1;
+    }
+    prob += gridDim.x;
+    if (prob < p.P) length = length_of(p, prob);
   }
 }
 
@@ -201,20 +204,29 @@ struct Ahead {
     const int page = p.cache.table[(int64_t)part.prob * p.cache.pitch + (t >> p.cache.shift)];
     pages = page < 0 ? 0 : page >= p.cache.n_blocks ? p.cache.n_blocks - 1 : page;
   }
-  // Address of the block's token base + of_lane in K or V; behind the row that of its last token.
-  __device__ __forceinline__ const char* address(const CacheAttnParams& p, const char* cache, int64_t s_block, int64_t s_head, int64_t s_token, int base,
-                                                 int of_lane) const {
-    const int in_block = (int)((1u << p.cache.shift) - 1u), page = __builtin_amdgcn_readlane(pages, (it * GPB + base / 16) & 63);
-    const int t = min(token0() + base + of_lane, part.row.len - 1) & in_block;
-    return cache + part.c * s_head + (int64_t)page * s_block + t * s_token;
+  // Group g of the block's groups of 16 tokens, in K or V: where its tokens begin, and how many of them lie behind the first (those behind the row are
+  // read as its last one).
+  struct Group {
+    const char* at;
+    int last;
+  };
+  __device__ __forceinline__ Group group(const CacheAttnParams& p, const char* cache, int64_t s_block, int64_t s_head, int64_t s_token, int g) const {
+    const int in_block = (int)((1u << p.cache.shift) - 1u), page = __builtin_amdgcn_readlane(pages, (it * GPB + g) & 63);
+    const int t = min(token0() + 16 * g, part.row.len - 1);
+    return {cache + part.c * s_head + page * s_block + (t & in_block) * s_token, part.row.len - 1 - t};
   }
-  __device__ __forceinline__ const char* key(const CacheAttnParams& p, int base, int of_lane) const {
-    return address(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, base, of_lane);
+  __device__ __forceinline__ Group keys(const CacheAttnParams& p, int g) const {
+    return group(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, g);
   }
-  __device__ __forceinline__ const char* value(const CacheAttnParams& p, int base, int of_lane) const {
-    return address(p, p.cache.V, p.cache.vs_block, p.cache.vs_head, p.cache.vs_token, base, of_lane);
+  __device__ __forceinline__ Group values(const CacheAttnParams& p, int g) const {
+    return group(p, p.cache.V, p.cache.vs_block, p.cache.vs_head, p.cache.vs_token, g);
   }
 };
+// The group's token t of this lane: a wave-uniform address and 32 bits per lane (a token's stride has less than 24).
+template <typename Group>
+__device__ __forceinline__ const char* token_at(const Group& g, int64_t s_token, int t, int offset) {
+  return g.at + (uint32_t)(__umul24((unsigned)min(t, g.last), (unsigned)s_token) + (unsigned)offset);
+}
 
 // ---- what becomes of a part ----------------------------------------------------------------------
 // In LDS a part is its accumulators [heads][D] and (max, sum) per head, not normalised.
@@ -243,39 +255,43 @@ __device__ __forceinline__ Left left_of(const CacheAttnParams& p, const Part<BT>
   return {g.prob * p.Hkv + g.c, g.block0, g.block1, g.row.n, g.row_end};
 }
 
-// The end of a workgroup, behind a barrier: its waves' parts, in order, those of a row merged.  acc(k), ml(k): part k, 2 w the
-// first one of wave w, 2 w + 1 its last one.
-template <int D, typename Acc, typename Ml>
-__device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Shares& shares, const Left (&left)[2 * NW], Acc acc, Ml ml) {
-  const int group = blockIdx.x, tid = threadIdx.x;
+// The end of a workgroup, behind a barrier: its waves' parts, in order, those of a row merged.  Part 2 w is the first one of wave w, 2 w + 1 its last
+// one; part k has its accumulators at acc + k * stride.
+template <int D, int HEADS>
+__device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Shares& shares, const Left (&left)[2 * NW], const float* acc, int stride,
+                                             const float2 (&ml)[2 * NW][HEADS]) {
+  const int group = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const float cexp = p.join_scale * 1.44269502162933349609375f;
-  for (int k0 = 0; k0 < 2 * NW;) {
-    const Left first = left[k0];
-    if (first.row < 0) {
-      ++k0;
-      continue;
-    }
-    unsigned set = 1u << k0;
-    int end = first.block1;
-    for (++k0; k0 < 2 * NW; ++k0) {
-      if (left[k0].row < 0) continue;
-      if (left[k0].row != first.row) break;
-      set |= 1u << k0;
-      end = left[k0].block1;
-    }
-    const bool begins = first.block0 == 0, whole = begins && end == first.n;
-    const int64_t head0 = (int64_t)first.row * p.G + p.g0, part0 = part_at(p, group, begins) + p.g0;
+  const Left mine = left[lane & (2 * NW - 1)];  // a part per lane
+  unsigned todo = (unsigned)__ballot(lane < 2 * NW && mine.row >= 0);
+  while (todo) {
+    const int k0 = __ffs(todo) - 1, row = __builtin_amdgcn_readlane(mine.row, k0), n = __builtin_amdgcn_readlane(mine.n, k0);
+    const unsigned set = todo & (unsigned)__ballot(mine.row == row);
+    const int last = __builtin_amdgcn_readlane(mine.block1, 31 - __clz(set));
+    todo &= ~set;
+    const bool begins = __builtin_amdgcn_readlane(mine.block0, k0) == 0, whole = begins && last == n;
+    const int64_t head0 = (int64_t)row * p.G + p.g0, part0 = part_at(p, group, begins) + p.g0;
     for (int i = tid; i < p.gb * D; i += NW * 64) {
       const int h = i / D;
-      float M = -INFINITY;
-      for (unsigned m = set; m; m &= m - 1) M = fmaxf(M, ml(__ffs(m) - 1)[h].x);
+      // all parts' numbers, whether they are the row's or not: what is not is left out by its factor
+      float2 v[2 * NW];
+      float x[2 * NW], M = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 2 * NW; ++k) {
+        v[k] = ml[k][h];
+        x[k] = acc[k * stride + i];
+      }
+#pragma unroll
+      for (int k = 0; k < 2 * NW; ++k) {
+        if (!(set >> k & 1)) v[k] = make_float2(-INFINITY, 0.f);
+        M = fmaxf(M, v[k].x);
+      }
       float a = 0.f, l = 0.f;
-      for (unsigned m = set; m; m &= m - 1) {
-        const int k = __ffs(m) - 1;
-        const float2 v = ml(k)[h];
-        const float f = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * cexp);
-        a += v.x == -INFINITY ? 0.f : acc(k)[i] * f;
-        l += v.y * f;
+#pragma unroll
+      for (int k = 0; k < 2 * NW; ++k) {
+        const float f = v[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v[k].x - M) * cexp);
+        a += v[k].x == -INFINITY ? 0.f : x[k] * f;
+        l += v[k].y * f;
       }
       if (whole) {
         p.out[head0 * D + i] = l == 0.f ? 0.f : a / l;
@@ -288,12 +304,12 @@ __device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Sha
     // Where a row's parts lie is said by the workgroup that begins it: a record per row (of rows without tokens by clear_empty), or, where there are
     // more rows than workgroups, one per workgroup.
     if (tid == 0 && begins && (!whole || p.by_row)) {
-      JoinRecord r = {first.row, -1, 0};
+      JoinRecord r = {row, -1, 0};
       if (!whole) {
         r.first = group;
-        r.last = shares.of(first.row_end - 1) / NW;
+        r.last = shares.of(__builtin_amdgcn_readlane(mine.row_end, k0) - 1) / NW;
       }
-      p.joins[p.by_row ? first.row : group] = r;
+      p.joins[p.by_row ? row : group] = r;
     }
   }
 }
@@ -371,17 +387,18 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
 // cost one product as they would with weights rounded to bf16, eight two, sixteen three.  (Rounded to bf16 the weights would put the outputs 1e-3 off, fp32's
 // own error is 1e-6, and the matrix cores have nothing else to do: four blocks of 128 dims are 64 KB, 2.5 us of HBM time for a CU.)
 template <int D, int GPAD>
-__global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
-  constexpr int BT = 32;
-  constexpr int CH = D / 8, TPL = 64 / CH, NLOAD = BT / TPL, KSTEPS = D / 32, ROWB = D * 2;
+__global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
+  constexpr int BT = attn_block(DT_BF16, D);
+  constexpr int CH = D / 8, TPL = 64 / CH, NLOAD = BT / TPL, KSTEPS = D / 32;
   constexpr int TILES = 16 / GPAD, NT = BT / 16;     // tiles of 16 tokens a q.K accumulator has slots for, tiles of a block
   constexpr int NACC = NT > TILES ? NT / TILES : 1;  // q.K accumulators of a block
   constexpr int NDT = D / 16;                        // output tiles of 16 dims
   constexpr int NSET = GPAD == 4 ? 1 : GPAD == 8 ? 2 : 3;  // A operands of the second product
-  static_assert(GPAD * D * 4 <= BT * ROWB, "a wave's accumulators fit its staging buffer");
-  __shared__ uint4 kbuf[NW][BT * CH];
+  // per wave: accumulators of its first part; staging buffer, at the end the accumulators of its last part.  (Part k's are at lds + k * kSpan.)
+  constexpr int kSpan = BT * CH;  // 16-byte units
+  static_assert(GPAD * D * 4 <= kSpan * 16, "a part's accumulators fit a staging buffer");
+  __shared__ uint4 lds[NW][2][kSpan];
   __shared__ __attribute__((aligned(16))) unsigned short pT[NW][NSET * 16][BT];  // parts of the weights, [part, head][token]
-  __shared__ __attribute__((aligned(16))) float s_first[NW][GPAD * D];  // accumulators of the waves' first parts
   __shared__ float2 s_ml[2 * NW][GPAD];
   __shared__ Left s_left[2 * NW];
 
@@ -391,14 +408,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
   const int number = blockIdx.x * NW + wave, g0 = p.g0, gb = p.gb;
   if (tid == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
   if (lane < 2) s_left[2 * wave + lane].row = -1;
+  const int empty = length_of(p, min((int)blockIdx.x, p.P - 1));
   Ahead<BT> ahead;
   const Shares shares = ahead.walk.start(p, number, lane);
   ahead.start();
   ahead.step(p, lane);
 
-  uint4* buf = kbuf[wave];
+  uint4* buf = lds[wave][1];
 #pragma unroll
-  for (int i = 0; i < NSET; ++i) reinterpret_cast<uint4*>(&pT[wave][16 * i][0])[lane] = make_uint4(0u, 0u, 0u, 0u);  // rows nobody writes stay 0
+  for (int i = 0; i < NSET * 16 * BT / 512; ++i) reinterpret_cast<uint4*>(&pT[wave][0][0])[i * 64 + lane] = make_uint4(0u, 0u, 0u, 0u);  // rows nobody writes stay 0
   const int hbase = (4 * j) % GPAD, tslot = (4 * j) / GPAD;  // this lane's heads and tile among a q.K accumulator's rows
   const float cexp = p.scale * 1.44269502162933349609375f;
   auto vswz = [](int t) { return CH == 16 ? (((t & 3) << 1) | (((t >> 3) & 1) << 3)) : ((t & 3) << 1); };
@@ -414,11 +432,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
   };
   auto load_k = [&] {
 #pragma unroll
-    for (int i = 0; i < NLOAD; ++i) kv[i] = ld16_stream(ahead.key(p, i * TPL, tq) + cl * 16);
+    for (int g = 0; g < BT / 16; ++g) {
+      const auto at = ahead.keys(p, g);
+#pragma unroll
+      for (int i = 0; i < 16 / TPL; ++i) kv[g * (16 / TPL) + i] = ld16_stream(token_at(at, p.cache.ks_token, i * TPL + tq, cl * 16));
+    }
   };
   auto load_v = [&] {
 #pragma unroll
-    for (int i = 0; i < NLOAD; ++i) vv[i] = ld16_stream(ahead.value(p, i * TPL, tq) + cl * 16);
+    for (int g = 0; g < BT / 16; ++g) {
+      const auto at = ahead.values(p, g);
+#pragma unroll
+      for (int i = 0; i < 16 / TPL; ++i) vv[g * (16 / TPL) + i] = ld16_stream(token_at(at, p.cache.vs_token, i * TPL + tq, cl * 16));
+    }
   };
   float m_run[4], l_part[4];
   f32x4_t acc[NDT];
@@ -462,7 +488,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
       f32x4_t d = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kc = 0; kc < KSTEPS; ++kc) {
-        const uint4 bb = buf[t * CH + ((4 * kc + j) ^ (n & (CH - 1)))];
+        const uint4 bb = buf[t * CH + ((4 * kc + j) ^ (t & (CH - 1)))];
         d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, qa[kc]), __builtin_bit_cast(bf16x8_t, bb), d, 0, 0, 0);
       }
 #pragma unroll
@@ -524,27 +550,37 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (ahead.valid) load_v();
 
-    uint4 pa[NSET];
+    uint4 pa[BT / 32][NSET];
 #pragma unroll
-    for (int i = 0; i < NSET; ++i) pa[i] = *reinterpret_cast<const uint4*>(&pT[wave][16 * i + n][8 * j]);
+    for (int kt = 0; kt < BT / 32; ++kt)
+#pragma unroll
+      for (int i = 0; i < NSET; ++i) pa[kt][i] = *reinterpret_cast<const uint4*>(&pT[wave][16 * i + n][32 * kt + 8 * j]);
+    // row 4j + r belongs to head hbase + r whatever part it is
+    if (__ballot(corr[0] != 1.f || corr[1] != 1.f || corr[2] != 1.f || corr[3] != 1.f)) {
+#pragma unroll
+      for (int nd = 0; nd < NDT; ++nd)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[nd][r] *= corr[r];
+    }
 #pragma unroll
     for (int nd = 0; nd < NDT; ++nd) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) acc[nd][r] *= corr[r];  // row 4j + r belongs to head hbase + r whatever part it is
       // transposed read: lane s of 16 gives the address of 4 dims of token s / 4 and receives its own dim of 4 tokens
       typedef short v4s_t __attribute__((ext_vector_type(4)));
-      const int tu = 8 * j + (n >> 2);
-      const int cch = (2 * nd + ((n & 3) >> 1)) ^ vswz(tu);  // vswz(tu) = vswz(tu + 4)
       const unsigned short* b16 = reinterpret_cast<const unsigned short*>(buf);
-      const v4s_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) v4s_t*)(b16 + (tu * CH + cch) * 8 + (n & 1) * 4));
-      const v4s_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) v4s_t*)(b16 + ((tu + 4) * CH + cch) * 8 + (n & 1) * 4));
-      struct { v4s_t a, b; } pair = {x0, x1};
-      const uint4 vb = __builtin_bit_cast(uint4, pair);
 #pragma unroll
-      for (int i = 0; i < NSET; ++i)
-        acc[nd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pa[i]), __builtin_bit_cast(bf16x8_t, vb), acc[nd], 0, 0, 0);
+      for (int kt = 0; kt < BT / 32; ++kt) {
+        const int tu = 32 * kt + 8 * j + (n >> 2);
+        const int cch = (2 * nd + ((n & 3) >> 1)) ^ vswz(tu);  // vswz(tu) = vswz(tu + 4)
+        const v4s_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) v4s_t*)(b16 + (tu * CH + cch) * 8 + (n & 1) * 4));
+        const v4s_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) v4s_t*)(b16 + ((tu + 4) * CH + cch) * 8 + (n & 1) * 4));
+        struct { v4s_t a, b; } pair = {x0, x1};
+        const uint4 vb = __builtin_bit_cast(uint4, pair);
+#pragma unroll
+        for (int i = 0; i < NSET; ++i)
+          acc[nd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pa[kt][i]), __builtin_bit_cast(bf16x8_t, vb), acc[nd], 0, 0, 0);
+      }
     }
 
     if (!last) continue;
@@ -559,7 +595,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
       if (GPAD <= 8) ls = swap32_sum(ls);
       if (n == 0 && j < GPAD / 4) s_ml[k][hbase + r] = make_float2(m_run[r], ls);
     }
-    float* s_acc = first ? s_first[wave] : reinterpret_cast<float*>(buf);  // [GPAD][D]
+    float* s_acc = reinterpret_cast<float*>(lds[wave][!first]);  // [GPAD][D]
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int nd = 0; nd < NDT; ++nd)
@@ -571,16 +607,21 @@ __global__ __launch_bounds__(256, 2) void cache_attn_bf16_kernel(CacheAttnParams
           a = swap16_sum(a);
         }
         if (GPAD <= 8) a = swap32_sum(a);
-        if (4 * j < GPAD) s_acc[(4 * j + r) * D + nd * 16 + n] = a;
+        acc[nd][r] = a;
       }
+    if (4 * j < GPAD) {
+#pragma unroll
+      for (int nd = 0; nd < NDT; ++nd)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s_acc[(4 * j + r) * D + nd * 16 + n] = acc[nd][r];
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (whole) write_row<BT, D>(p, part, lane, s_acc, s_ml[k]);
     reset();
   }
   __syncthreads();
-  finish_group<D>(p, shares, s_left, [&](int k) { return k & 1 ? reinterpret_cast<const float*>(kbuf[k >> 1]) : s_first[k >> 1]; },
-                  [&](int k) { return s_ml[k]; });
-  if (g0 == 0) clear_empty(p);
+  finish_group<D, GPAD>(p, shares, s_left, reinterpret_cast<const float*>(&lds[0][0][0]), kSpan * 4, s_ml);
+  if (g0 == 0) clear_empty(p, empty);
 }
 
 // fp32 caches.  Both products and the sums in fp64 (an fp32 logit of magnitude 100 would be off by 2.5e-5, and so would its softmax weight);
@@ -607,6 +648,7 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   const int number = blockIdx.x * NW + wave, g0 = p.g0;
   if (tid == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
   if (lane < 2) s_left[2 * wave + lane].row = -1;
+  const int empty = length_of(p, min((int)blockIdx.x, p.P - 1));
   Ahead<BT> ahead;
   const Shares shares = ahead.walk.start(p, number, lane);
   ahead.start();
@@ -617,14 +659,14 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   auto load_k = [&] {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const char* a = ahead.key(p, 8 * g, t8) + sl * 16;
+      const char* a = token_at(ahead.keys(p, g / 2), p.cache.ks_token, g % 2 * 8 + t8, sl * 16);
 #pragma unroll
       for (int ch = 0; ch < NC; ++ch) kv[g][ch] = ld16(a + ch * 128);
     }
   };
   auto load_v = [&] {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) vv[i] = ld16(ahead.value(p, i * TPL, tq) + cl * 16);
+    for (int i = 0; i < NV; ++i) vv[i] = ld16(token_at(ahead.values(p, i * TPL / 16), p.cache.vs_token, i * TPL % 16 + tq, cl * 16));
   };
   constexpr int NQ = (GB * D + 63) / 64;
   float qv[NQ];  // the next part's queries
@@ -777,8 +819,8 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
     if (ahead.valid) keep_q();
   }
   __syncthreads();
-  finish_group<D>(p, shares, s_left, [&](int k) { return s_acc[k]; }, [&](int k) { return s_ml[k]; });
-  if (g0 == 0) clear_empty(p);
+  finish_group<D, GB>(p, shares, s_left, &s_acc[0][0], GB * D, s_ml);
+  if (g0 == 0) clear_empty(p, empty);
 }
 
 template <int D, int GB = 1>

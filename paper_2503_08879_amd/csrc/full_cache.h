@@ -33,8 +33,8 @@ struct RotaryParams {
 };
 hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
 
-constexpr int kAttnGroups = 512;  // workgroups of an attention launch at most: two per CU,
-constexpr int kAttnWaves = 2048;  // of four waves
+constexpr int kAttnGroups = 256;  // workgroups of an attention launch at most: two per CU,
+constexpr int kAttnWaves = 1024;  // of four waves
 constexpr int kRowWeight = 1;     // a row's beginning and end, in blocks
 
 // A row whose parts are to be joined, those of workgroups first (its second slot) and first + 1 .. last (their first slots).
@@ -42,8 +42,8 @@ struct JoinRecord {
   int row, first, last;  // first < 0: nothing to do
 };
 
-// Tokens of a block: 16 KB of K and V are in flight for a wave.
-inline int attn_block(int dtype, int head_dim) { return dtype == 1 && head_dim == 128 ? 16 : 32; }
+// Tokens of a block.
+constexpr int attn_block(int dtype, int head_dim) { return dtype == 1 ? (head_dim == 128 ? 16 : 32) : (head_dim == 128 ? 32 : 64); }
 
 struct CacheAttnParams {
   FullCache cache;

@@ -152,7 +152,7 @@ CACHE_REFUSALS = [
     (INVALID, True, dict(block_table=None)), (UNSUPPORTED, True, dict(block_table=P16 + 2)), (INVALID, True, dict(n_pages=0)),
     (INVALID, True, dict(page_size=8)), (INVALID, True, dict(page_size=48)), (INVALID, True, dict(table_pitch=6)),
     (UNSUPPORTED, True, dict(k_stride_page=4100)), (UNSUPPORTED, True, dict(v_stride_page=-4096)), (UNSUPPORTED, True, dict(k_stride_token=64)),
-    (UNSUPPORTED, False, dict(v_stride_head=12)), (INVALID, True, dict(K=None)), (INVALID, True, dict(V=None)),
+    (UNSUPPORTED, False, dict(v_stride_head=12)), (UNSUPPORTED, False, dict(k_stride_token=1 << 23)), (UNSUPPORTED, True, dict(v_stride_token=1 << 23)), (INVALID, True, dict(K=None)), (INVALID, True, dict(V=None)),
     (UNSUPPORTED, True, dict(K=P16 + 8)), (UNSUPPORTED, True, dict(V=P16 + 8)), (INVALID, True, dict(lens=None)),
     (UNSUPPORTED, True, dict(lens=P16 + 1)),
 ]
@@ -216,7 +216,7 @@ def test_attn_workspace():
     n = fc._fn("sagekvc_attn_workspace_bytes")
     assert n(None) == 0
     desc = sk.CacheDesc(3, 8, 2, 128, sk.BF16, 100, 0, 0, 0, 0, 0, 0)  # strides do not enter
-    assert n(byref(desc)) == 2 * 512 * 4 * (128 * 4 + 8) + 512 * 12
+    assert n(byref(desc)) == 2 * 256 * 4 * (128 * 4 + 8) + 256 * 12
     desc.head_dim = 96
     assert n(byref(desc)) == 0
 
