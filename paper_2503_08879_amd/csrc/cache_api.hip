@@ -113,8 +113,8 @@ sagekv_status check_cache(const sagekvc_desc* d, const sagekv_paged_kv* pg, cons
   const int eb = element_bytes(d->dtype);
   c->K = (char*)const_cast<void*>(K);
   c->V = (char*)const_cast<void*>(V);
-  c->ks_block = k[0] * eb, c->ks_head = k[1] * eb, c->ks_token = k[2] * eb;
-  c->vs_block = v[0] * eb, c->vs_head = v[1] * eb, c->vs_token = v[2] * eb;
+  c->ks_block = k[0] * eb, c->ks_head = k[1] * eb, c->ks_token = (int)k[2] * eb;
+  c->vs_block = v[0] * eb, c->vs_head = v[1] * eb, c->vs_token = (int)v[2] * eb;
   return SAGEKV_OK;
 }
 
@@ -278,18 +278,15 @@ sagekv_status sagekvc_attn(const sagekvc_desc* d, const sagekv_paged_kv* pages, 
     const int64_t ends = (p.S + bt - 1) / bt + (p.W + bt - 2) / bt + 1;
     if (ends < blocks) blocks = ends;
   }
-  // Rows of up to 256 tokens are not worth a join: a workgroup's four waves take a row together, or, where there are more rows than workgroups, a wave
-  // takes it alone.
-  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads;
-  p.row_parts = blocks * bt > 256 ? 0 : rows <= kAttnGroups ? 4 : 1;
-  const int64_t weight = rows * (p.row_parts ? p.row_parts : blocks + kRowWeight);
+  const int64_t rows = (int64_t)d->n_problems * d->n_kv_heads, weight = rows * (blocks + 4);
   if (weight > 0x7FFFFFFF) return SAGEKV_ERR_UNSUPPORTED;
   p.n_waves = weight < kAttnWaves ? (int)weight : kAttnWaves;
   p.by_row = rows <= kAttnGroups;
   p.part_acc = (float*)((char*)workspace + l.acc);
   p.part_ml = (float2*)((char*)workspace + l.ml);
   p.joins = (JoinRecord*)((char*)workspace + l.joins);
-  return dev(launch_cache_attn(p, p.row_parts == 0, (hipStream_t)hip_stream));
+  const bool short_rows = RowCuts(rows).rounds(blocks) <= kWholeRounds;  // none will be split, whatever the lengths are
+  return dev(launch_cache_attn(p, !short_rows, (hipStream_t)hip_stream));
 }
 
 }  // extern "C"

@@ -49,10 +49,6 @@ struct RowBlocks {
     }
   }
 };
-__device__ __forceinline__ int weight_of(const CacheAttnParams& p, int blocks) {
-  return blocks == 0 ? 0 : p.row_parts ? p.row_parts : blocks + kRowWeight;
-}
-
 // The shares: `more` of them of size + 1, the others of size.
 struct Shares {
   int n, size, more;
@@ -64,72 +60,84 @@ struct Shares {
   }
 };
 
-// A part of a row, blocks [block0, block1).
-template <int BT>
-struct Part {
-  int prob, c, block0, block1;
-  RowBlocks<BT> row;
-  int row_end;  // in weights, from the first row's beginning
-};
-
-// Weight of n problems (of a row of each); *one: the length, if it is one.
-template <int BT>
-__device__ __forceinline__ int weights_of(const CacheAttnParams& p, int first, int n, int* one) {
-  int sum = 0;
-  for (int i0 = 0; i0 < n; i0 += 4) {
-    int len[4];
+// What n problems have: blocks, problems with tokens, the most blocks (of one row of each problem); and the last one's length.
+struct Census {
+  int blocks, rows, most, length;
+  template <int BT>
+  __device__ __forceinline__ void take(const CacheAttnParams& p, int first, int n) {
+    blocks = rows = most = length = 0;
+    for (int i0 = 0; i0 < n; i0 += 4) {
+      int len[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) len[i] = p.lens[first + min(i0 + i, n - 1)];
-    *one = len[0];
+      for (int i = 0; i < 4; ++i) len[i] = p.lens[first + min(i0 + i, n - 1)];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sum += i0 + i < n ? weight_of(p, RowBlocks<BT>(p, len[i]).n) : 0;
+      for (int i = 0; i < 4; ++i) {
+        const int b = i0 + i < n ? RowBlocks<BT>(p, len[i]).n : 0;
+        blocks += b;
+        rows += b > 0;
+        most = max(most, b);
+      }
+      length = len[3];
+    }
   }
-  return sum;
-}
+};
 
 // A wave's share, part by part.
 template <int BT>
 struct Walk {
   int at, end;        // what is left of it, in weights
+  int cuts;           // > 0: every row weighs that much, and each unit of its weight is an equal part of it
   int prob, c, done;  // the row that `at` is in, and what of its weight lies before
   RowBlocks<BT> row;
+  __device__ __forceinline__ int weight() const { return row.n == 0 ? 0 : cuts ? cuts : row.n + kRowWeight; }
   // wave: its number in the launch
   __device__ __forceinline__ Shares start(const CacheAttnParams& p, int wave, int lane) {
-    int lo = 0, n = p.P, before = 0, length = 0;
+    int lo = 0, n = p.P, before = 0;
     Shares shares(0, 1);
     bool counted = false;
     at = end = 0;
     for (;;) {  // a problem out of 64, of 64 * 64, ...
       const int per = (n + 63) / 64, first = lane * per, mine = max(0, min(per, n - first));
-      const int incl = wave_scan_incl(weights_of<BT>(p, lo + first, mine, &length)) * p.Hkv;
+      Census census;
+      census.take<BT>(p, lo + first, mine);
+      const int blocks = wave_scan_incl(census.blocks) * p.Hkv, rows = wave_scan_incl(census.rows) * p.Hkv;
       if (!counted) {
         counted = true;
-        const int total = __builtin_amdgcn_readlane(incl, 63);
-        shares = Shares(total, max(1, min(total, p.n_waves)));
-        if (wave >= min(total, p.n_waves)) return shares;
+        const int all_blocks = __builtin_amdgcn_readlane(blocks, 63), all_rows = __builtin_amdgcn_readlane(rows, 63);
+        // Whole rows, a workgroup's, two waves' or a wave's each, where the longest one takes hardly longer than an even share of all blocks does: parts of rows
+        // to be joined cost about four rounds.  (256 rows of 7 heads x 128 dims, us, split and whole: 260 tokens 20.5 14.0, 512 26.5 16.8, 768 31.7 22.1; 8 rows of
+        // 4 heads: 260 12.3 12.0, 384 12.1 12.0, 512 12.0 14.0, 768 12.0 17.9.)
+        const RowCuts whole(all_rows);
+        cuts = whole.rounds(wave_max_i(census.most)) <= all_blocks / kAttnWaves + kWholeRounds ? whole.cuts : 0;
+        const int total = cuts ? all_rows * cuts : all_blocks + all_rows * kRowWeight, busy = min(total, p.n_waves);
+        shares = Shares(total, max(1, busy));
+        if (wave >= busy) return shares;
         at = shares.begin(wave);
         end = shares.begin(wave + 1);
       }
       // the first lane whose problems reach beyond the share's begin
+      const int incl = cuts ? rows * cuts : blocks + rows * kRowWeight;
       const int hit = __ffsll((unsigned long long)__ballot(before + incl > at)) - 1;
       before += hit > 0 ? __builtin_amdgcn_readlane(incl, hit - 1) : 0;
       lo += hit * per;
       n = min(per, n - hit * per);
       if (per > 1) continue;
-      row = RowBlocks<BT>(p, __builtin_amdgcn_readlane(length, hit));
+      row = RowBlocks<BT>(p, __builtin_amdgcn_readlane(census.length, hit));
       break;
     }
     prob = lo;
-    const int weight = weight_of(p, row.n), in_problem = at - before;
-    c = in_problem / weight;
-    done = in_problem - c * weight;
+    const int w = weight(), in_problem = at - before;
+    c = in_problem / w;
+    done = in_problem - c * w;
     return shares;
   }
+  int block0, block1;  // the part of that row: its blocks
+  int row_end;         // where the row ends, in weights
   // the next part that holds blocks; false: none is left
-  __device__ __forceinline__ bool next(const CacheAttnParams& p, Part<BT>* g) {
+  __device__ __forceinline__ bool next(const CacheAttnParams& p) {
     while (at < end) {
-      const int weight = weight_of(p, row.n);
-      if (done == weight) {
+      const int w = weight();
+      if (done == w) {
         done = 0;
         if (++c == p.Hkv) {
           c = 0;
@@ -138,19 +146,18 @@ struct Walk {
         }
         continue;
       }
-      const int take = min(weight - done, end - at);
-      g->prob = prob, g->c = c, g->row = row;
-      g->row_end = at - done + weight;
-      if (p.row_parts) {
-        g->block0 = row.n * done / p.row_parts;
-        g->block1 = row.n * (done + take) / p.row_parts;
+      const int take = min(w - done, end - at);
+      row_end = at - done + w;
+      if (cuts) {  // 1, 2 or 4
+        block0 = row.n * done / cuts;
+        block1 = row.n * (done + take) / cuts;
       } else {
-        g->block0 = max(done - kRowWeight, 0);
-        g->block1 = max(done + take - kRowWeight, 0);
+        block0 = max(done - kRowWeight, 0);
+        block1 = max(done + take - kRowWeight, 0);
       }
       at += take;
       done += take;
-      if (g->block1 > g->block0) return true;
+      if (block1 > block0) return true;
     }
     return false;
   }
@@ -181,27 +188,24 @@ struct Mask {
 
 // The block that a wave loads next.
 template <int BT>
-struct Ahead {
+struct Ahead : Walk<BT> {
   static constexpr int GPB = BT / 16;  // groups of 16 tokens of a block
-  Walk<BT> walk;
-  Part<BT> part;
-  int it, n;   // block `it` of the part's n
+  int it;      // block `it` of the part
   int pages;   // of the next 64 groups, one per lane (a dense cache's "page" is the problem)
   bool valid;  // there is a block
-  __device__ __forceinline__ int token0() const { return part.row.token(part.block0 + it); }
-  __device__ __forceinline__ void start() { valid = true, it = -1, n = 0; }
+  __device__ __forceinline__ int token0() const { return this->row.token(this->block0 + it); }
   __device__ __forceinline__ void step(const CacheAttnParams& p, int lane) {
-    if (++it >= n) {
-      valid = walk.next(p, &part);
+    if (this->block0 + ++it >= this->block1) {
+      valid = this->next(p);
       if (!valid) return;
       it = 0;
-      n = part.block1 - part.block0;
     }
     if ((it * GPB & 63) != 0) return;
-    pages = part.prob;
+    pages = this->prob;
     if (!p.cache.table) return;
-    const int t = min(part.row.token(part.block0 + min(it + lane / GPB, n - 1)) + lane % GPB * 16, part.row.len - 1);
-    const int page = p.cache.table[(int64_t)part.prob * p.cache.pitch + (t >> p.cache.shift)];
+    const int block = min(this->block0 + it + lane / GPB, this->block1 - 1);
+    const int t = min(this->row.token(block) + lane % GPB * 16, this->row.len - 1);
+    const int page = p.cache.table[(int64_t)this->prob * p.cache.pitch + (t >> p.cache.shift)];
     pages = page < 0 ? 0 : page >= p.cache.n_blocks ? p.cache.n_blocks - 1 : page;
   }
   // Group g of the block's groups of 16 tokens, in K or V: where its tokens begin, and how many of them lie behind the first (those behind the row are
@@ -210,10 +214,10 @@ struct Ahead {
     const char* at;
     int last;
   };
-  __device__ __forceinline__ Group group(const CacheAttnParams& p, const char* cache, int64_t s_block, int64_t s_head, int64_t s_token, int g) const {
+  __device__ __forceinline__ Group group(const CacheAttnParams& p, const char* cache, int64_t s_block, int64_t s_head, int s_token, int g) const {
     const int in_block = (int)((1u << p.cache.shift) - 1u), page = __builtin_amdgcn_readlane(pages, (it * GPB + g) & 63);
-    const int t = min(token0() + 16 * g, part.row.len - 1);
-    return {cache + part.c * s_head + page * s_block + (t & in_block) * s_token, part.row.len - 1 - t};
+    const int t = min(token0() + 16 * g, this->row.len - 1);
+    return {cache + this->c * s_head + page * s_block + (int64_t)(t & in_block) * s_token, this->row.len - 1 - t};
   }
   __device__ __forceinline__ Group keys(const CacheAttnParams& p, int g) const {
     return group(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, g);
@@ -224,7 +228,7 @@ struct Ahead {
 };
 // The group's token t of this lane: a wave-uniform address and 32 bits per lane (a token's stride has less than 24).
 template <typename Group>
-__device__ __forceinline__ const char* token_at(const Group& g, int64_t s_token, int t, int offset) {
+__device__ __forceinline__ const char* token_at(const Group& g, int s_token, int t, int offset) {
   return g.at + (uint32_t)(__umul24((unsigned)min(t, g.last), (unsigned)s_token) + (unsigned)offset);
 }
 
@@ -232,37 +236,33 @@ __device__ __forceinline__ const char* token_at(const Group& g, int64_t s_token,
 // In LDS a part is its accumulators [heads][D] and (max, sum) per head, not normalised.
 __device__ __forceinline__ int64_t part_at(const CacheAttnParams& p, int group, bool begins) { return ((int64_t)group * 2 + begins) * p.G; }
 
+// A part that a wave leaves in LDS: the first one of its share, or its last one.  row < 0: there is none.
+struct Part {
+  int row, block0, block1, n, row_end;  // of a row of n blocks
+  __device__ __forceinline__ bool whole() const { return block0 == 0 && block1 == n; }
+};
+
 // A row that a wave has for itself.
-template <int BT, int D>
-__device__ __forceinline__ void write_row(const CacheAttnParams& p, const Part<BT>& g, int lane, const float* acc, const float2* ml) {
-  const int row = g.prob * p.Hkv + g.c;
+template <int D>
+__device__ __forceinline__ void write_row(const CacheAttnParams& p, int row, int lane, const float* acc, const float2* ml) {
   const int64_t head0 = (int64_t)row * p.G + p.g0;
   for (int i = lane; i < p.gb * (D / 4); i += 64) {
-    const float l = ml[i / (D / 4)].y;
+    const float l = ml[i / (D / 4)].y, f = l == 0.f ? 0.f : 1.f / l;
     const float4 a = reinterpret_cast<const float4*>(acc)[i];
-    reinterpret_cast<float4*>(p.out + head0 * D)[i] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x / l, a.y / l, a.z / l, a.w / l);
+    reinterpret_cast<float4*>(p.out + head0 * D)[i] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
   }
   if (p.lse && lane < p.gb) p.lse[head0 + lane] = ml[lane].y == 0.f ? -INFINITY : fmaf(ml[lane].x, p.join_scale, logf(ml[lane].y));
   if (p.by_row && lane == 0) p.joins[row].first = -1;
 }
 
-// A part that a wave leaves in LDS: the first one of its share, or its last one.  row < 0: there is none.
-struct Left {
-  int row, block0, block1, n, row_end;  // as in Part
-};
-template <int BT>
-__device__ __forceinline__ Left left_of(const CacheAttnParams& p, const Part<BT>& g) {
-  return {g.prob * p.Hkv + g.c, g.block0, g.block1, g.row.n, g.row_end};
-}
-
 // The end of a workgroup, behind a barrier: its waves' parts, in order, those of a row merged.  Part 2 w is the first one of wave w, 2 w + 1 its last
 // one; part k has its accumulators at acc + k * stride.
 template <int D, int HEADS>
-__device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Shares& shares, const Left (&left)[2 * NW], const float* acc, int stride,
+__device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Shares& shares, const Part (&left)[2 * NW], const float* acc, int stride,
                                              const float2 (&ml)[2 * NW][HEADS]) {
   const int group = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const float cexp = p.join_scale * 1.44269502162933349609375f;
-  const Left mine = left[lane & (2 * NW - 1)];  // a part per lane
+  const Part mine = left[lane & (2 * NW - 1)];  // a part per lane
   unsigned todo = (unsigned)__ballot(lane < 2 * NW && mine.row >= 0);
   while (todo) {
     const int k0 = __ffs(todo) - 1, row = __builtin_amdgcn_readlane(mine.row, k0), n = __builtin_amdgcn_readlane(mine.n, k0);
@@ -314,36 +314,68 @@ __device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Sha
   }
 }
 
-// Merges the parts of a row that were left in scratch: a workgroup per (record, head).
+// Merges the parts of a row that were left in scratch: a workgroup per (record, head), or, where there are few parts, a wave per head.
 template <int D>
 __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
   constexpr int C4 = D / 4, Q = 256 / C4, U = 8;  // lanes per part (16 bytes each), parts at a time, rounds in flight at the start
-  __shared__ float factor[kAttnWaves / NW];
+  __shared__ float factor[kAttnGroups];
   __shared__ float4 sums[Q][C4];
   __shared__ float s_max[4];
   __shared__ double s_den[4];
   const JoinRecord r = p.joins[blockIdx.x];
   if (r.first < 0) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = blockIdx.y, q = tid / C4, j = tid % C4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = r.last - r.first + 1;
+  const float c = p.join_scale * 1.44269502162933349609375f;
+  auto finish = [&](int g, int j, float num, double den, float M) {  // dim j of head g
+    const int64_t head = (int64_t)r.row * p.G + g;
+    p.out[head * D + j] = den == 0.0 ? 0.f : num / (float)den;
+    if (p.lse && j == 0) p.lse[head] = den == 0.0 ? -INFINITY : fmaf(M, p.join_scale, logf((float)den));
+  };
+  if (n <= U) {
+    const int g = blockIdx.y * 4 + wave;
+    if (g < p.G) {
+      auto part = [&](int s) { return part_at(p, r.first + s, s == 0) + g; };
+      const float2 v = lane < n ? p.part_ml[part(lane)] : make_float2(-INFINITY, 0.f);
+      float2 a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[u] = lane < D / 2 ? reinterpret_cast<const float2*>(p.part_acc + part(min(u, n - 1)) * D)[lane] : make_float2(0.f, 0.f);
+      const float M = wave_combine<true, 1>(v.x);
+      const float f = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * c);
+      const double den = group_sum_f64<64>((double)v.y * f);
+      float2 num = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float fu = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), u));  // 0 behind the last part
+        if (fu == 0.f) continue;
+        num.x = fmaf(a[u].x, fu, num.x);
+        num.y = fmaf(a[u].y, fu, num.y);
+      }
+      if (lane < D / 2) {
+        finish(g, 2 * lane, num.x, den, M);
+        finish(g, 2 * lane + 1, num.y, den, M);
+      }
+    }
+    return;
+  }
+  const int q = tid / C4, j = tid % C4, g = blockIdx.y;
   auto part = [&](int s) { return part_at(p, r.first + s, s == 0) + g; };
   auto acc = [&](int s) { return reinterpret_cast<const float4*>(p.part_acc)[part(s) * C4 + j]; };
   float4 early[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) early[u] = acc(min(q + u * Q, n - 1));
-  // the parts' factors; one without weight (all of its logits -infinity) is left out
-  const float c = p.join_scale * 1.44269502162933349609375f;
   float M = -INFINITY;
   for (int s = tid; s < n; s += 256) M = fmaxf(M, p.part_ml[part(s)].x);
   M = wave_combine<true, 1>(M);
   if (lane == 0) s_max[wave] = M;
   __syncthreads();
   M = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+  // the parts' factors; one without weight (all of its logits -infinity) is left out
   double den = 0.0;
   for (int s = tid; s < n; s += 256) {
     const float2 v = p.part_ml[part(s)];
     const float f = v.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((v.x - M) * c);
-    factor[s] = v.x == -INFINITY ? -1.f : f;
+    factor[s] = f;
     den += (double)v.y * f;
   }
   den = group_sum_f64<64>(den);
@@ -352,7 +384,7 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
   den = (s_den[0] + s_den[1]) + (s_den[2] + s_den[3]);
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](const float4& v, float f) {
-    if (f < 0.f) return;
+    if (f == 0.f) return;
     a.x = fmaf(v.x, f, a.x), a.y = fmaf(v.y, f, a.y), a.z = fmaf(v.z, f, a.z), a.w = fmaf(v.w, f, a.w);
   };
 #pragma unroll
@@ -360,24 +392,20 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
     if (q + u * Q < n) add(early[u], factor[q + u * Q]);
   for (int s0 = q + U * Q; s0 < n; s0 += 4 * Q) {
     float4 v[4];
-    float f[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      f[u] = s0 + u * Q < n ? factor[s0 + u * Q] : -1.f;
-      if (f[u] >= 0.f) v[u] = acc(s0 + u * Q);
-    }
+    for (int u = 0; u < 4; ++u) v[u] = acc(min(s0 + u * Q, n - 1));
 #pragma unroll
-    for (int u = 0; u < 4; ++u) add(v[u], f[u]);
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u * Q < n) add(v[u], factor[s0 + u * Q]);
   }
   sums[q][j] = a;
   __syncthreads();
-  if (tid >= D) return;
-  float num = 0.f;
+  if (tid < D) {
+    float num = 0.f;
 #pragma unroll
-  for (int i = 0; i < Q; ++i) num += reinterpret_cast<const float*>(&sums[i][0])[tid];
-  const int64_t head = (int64_t)r.row * p.G + g;
-  p.out[head * D + tid] = den == 0.0 ? 0.f : num / (float)den;
-  if (p.lse && tid == 0) p.lse[head] = den == 0.0 ? -INFINITY : fmaf(M, p.join_scale, logf((float)den));
+    for (int i = 0; i < Q; ++i) num += reinterpret_cast<const float*>(&sums[i][0])[tid];
+    finish(g, tid, num, den, M);
+  }
 }
 
 // bf16 caches.  A wave takes 32 tokens at a time: K goes through the wave's staging buffer in LDS (16-byte chunks, XOR-swizzled) into
@@ -400,7 +428,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
   __shared__ uint4 lds[NW][2][kSpan];
   __shared__ __attribute__((aligned(16))) unsigned short pT[NW][NSET * 16][BT];  // parts of the weights, [part, head][token]
   __shared__ float2 s_ml[2 * NW][GPAD];
-  __shared__ Left s_left[2 * NW];
+  __shared__ Part s_left[2 * NW];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tq = lane / CH, cl = lane % CH;  // load role: token of a load, 16-byte chunk
@@ -410,8 +438,8 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
   if (lane < 2) s_left[2 * wave + lane].row = -1;
   const int empty = length_of(p, min((int)blockIdx.x, p.P - 1));
   Ahead<BT> ahead;
-  const Shares shares = ahead.walk.start(p, number, lane);
-  ahead.start();
+  const Shares shares = ahead.start(p, number, lane);
+  ahead.it = -1, ahead.block0 = ahead.block1 = 0;
   ahead.step(p, lane);
 
   uint4* buf = lds[wave][1];
@@ -455,15 +483,15 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
     for (int nd = 0; nd < NDT; ++nd) acc[nd] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   };
   if (ahead.valid) {
-    load_q(ahead.part.prob, ahead.part.c);
+    load_q(ahead.prob, ahead.c);
     load_k();
     load_v();
     reset();
   }
   while (ahead.valid) {
-    const Part<BT> part = ahead.part;
+    const Part part = {ahead.prob * p.Hkv + ahead.c, ahead.block0, ahead.block1, ahead.row.n, ahead.row_end};
     const int t0 = ahead.token0();
-    const Mask mask(p, part.row.len);
+    const Mask mask(p, ahead.row.len);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of the buffer are done
 #pragma unroll
     for (int i = 0; i < NLOAD; ++i) {
@@ -494,7 +522,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[ts / TILES][r] = ts % TILES == 0 || tslot == ts % TILES ? d[r] : x[ts / TILES][r];
     }
-    if (last && ahead.valid) load_q(ahead.part.prob, ahead.part.c);
+    if (last && ahead.valid) load_q(ahead.prob, ahead.c);
 #pragma unroll
     for (int a = 0; a < NACC; ++a) {
       const int tile = a * TILES + tslot;
@@ -585,9 +613,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
 
     if (!last) continue;
     // the part's totals: weights over the lanes that share a head, accumulators over the rows that hold its parts
-    const bool whole = part.block0 == 0 && part.block1 == part.row.n, first = !whole && ahead.valid;
+    const bool whole = part.whole(), first = !whole && ahead.valid;
     const int k = 2 * wave + !first;
-    if (!whole && lane == 0) s_left[k] = left_of(p, part);
+    if (!whole && lane == 0) s_left[k] = part;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float ls = group_sum<16>(l_part[r]);
@@ -616,7 +644,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
         for (int r = 0; r < 4; ++r) s_acc[(4 * j + r) * D + nd * 16 + n] = acc[nd][r];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (whole) write_row<BT, D>(p, part, lane, s_acc, s_ml[k]);
+    if (whole) write_row<D>(p, part.row, lane, s_acc, s_ml[k]);
     reset();
   }
   __syncthreads();
@@ -640,7 +668,7 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   __shared__ __attribute__((aligned(16))) double pw[NW][BT][GP];
   __shared__ __attribute__((aligned(16))) float s_acc[2 * NW][GB * D];
   __shared__ float2 s_ml[2 * NW][GB];
-  __shared__ Left s_left[2 * NW];
+  __shared__ Part s_left[2 * NW];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int t8 = lane >> 3, sl = lane & 7;   // K role: token of a group, share of a token; head, once the logits are summed
@@ -650,8 +678,8 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   if (lane < 2) s_left[2 * wave + lane].row = -1;
   const int empty = length_of(p, min((int)blockIdx.x, p.P - 1));
   Ahead<BT> ahead;
-  const Shares shares = ahead.walk.start(p, number, lane);
-  ahead.start();
+  const Shares shares = ahead.start(p, number, lane);
+  ahead.it = -1, ahead.block0 = ahead.block1 = 0;
   ahead.step(p, lane);
 
   double* qd = s_q[wave];
@@ -692,16 +720,16 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
       for (int e = 0; e < 4; ++e) acc[g][e] = 0.0;
   };
   if (ahead.valid) {
-    load_q(ahead.part.prob, ahead.part.c);
+    load_q(ahead.prob, ahead.c);
     load_k();
     if (!LATE_V) load_v();
     reset();
     keep_q();
   }
   while (ahead.valid) {
-    const Part<BT> part = ahead.part;
+    const Part part = {ahead.prob * p.Hkv + ahead.c, ahead.block0, ahead.block1, ahead.row.n, ahead.row_end};
     const int t0 = ahead.token0();
-    const Mask mask(p, part.row.len);
+    const Mask mask(p, ahead.row.len);
     const bool cut = mask.cuts(t0, BT);
     double x[NG];  // of head sl, token 8 g + t8
 #pragma unroll
@@ -795,10 +823,10 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
 
     if (!last) continue;
     // the part's totals: over the lanes that share a chunk of V, and those that share a head
-    if (ahead.valid) load_q(ahead.part.prob, ahead.part.c);
-    const bool whole = part.block0 == 0 && part.block1 == part.row.n, first = !whole && ahead.valid;
+    if (ahead.valid) load_q(ahead.prob, ahead.c);
+    const bool whole = part.whole(), first = !whole && ahead.valid;
     const int k = 2 * wave + !first;
-    if (!whole && lane == 0) s_left[k] = left_of(p, part);
+    if (!whole && lane == 0) s_left[k] = part;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int g = 0; g < GB; ++g)
@@ -814,7 +842,7 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
     l = swap32_sum_f64(l);
     if (lane < GB) s_ml[k][lane] = make_float2(m, (float)l);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (whole) write_row<BT, D>(p, part, lane, s_acc[k], s_ml[k]);
+    if (whole) write_row<D>(p, part.row, lane, s_acc[k], s_ml[k]);
     reset();
     if (ahead.valid) keep_q();
   }

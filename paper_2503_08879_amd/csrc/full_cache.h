@@ -15,7 +15,8 @@ struct TokenRows {
 // the problem itself (table null, shift 31) or table[p * pitch + (t >> shift)].
 struct FullCache {
   char *K, *V;
-  int64_t ks_block, ks_head, ks_token, vs_block, vs_head, vs_token;
+  int64_t ks_block, ks_head, vs_block, vs_head;
+  int ks_token, vs_token;  // less than 2^24
   const int32_t* table;
   int64_t pitch;
   int shift, n_blocks;
@@ -33,9 +34,18 @@ struct RotaryParams {
 };
 hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
 
-constexpr int kAttnGroups = 256;  // workgroups of an attention launch at most: two per CU,
-constexpr int kAttnWaves = 1024;  // of four waves
-constexpr int kRowWeight = 1;     // a row's beginning and end, in blocks
+constexpr int kAttnGroups = 256;   // workgroups of an attention launch at most: one per CU,
+constexpr int kAttnWaves = 1024;   // of four waves
+constexpr int kRowWeight = 2;      // a row's beginning and end, in blocks
+constexpr int kWholeRounds = 3;    // see Walk::start in cache_attn.hip
+
+// Whole rows: how many waves each gets, and how many blocks the longest row's waves then take one after the other, at most.
+struct RowCuts {
+  int cuts, rows_each;
+  __host__ __device__ explicit RowCuts(int64_t rows)
+      : cuts(4 * rows <= kAttnWaves ? 4 : 2 * rows <= kAttnWaves ? 2 : 1), rows_each((int)((rows * cuts + kAttnWaves - 1) / kAttnWaves)) {}
+  __host__ __device__ int64_t rounds(int64_t blocks) const { return (blocks + cuts - 1) / cuts * rows_each; }
+};
 
 // A row whose parts are to be joined, those of workgroups first (its second slot) and first + 1 .. last (their first slots).
 struct JoinRecord {
@@ -52,8 +62,7 @@ struct CacheAttnParams {
   const int32_t* lens;
   int P, Hq, Hkv, G, D, dtype;
   int S, W, max_len;
-  int row_parts;  // short rows: each is split into that many parts, whatever its length; else 0
-  bool by_row;    // a join record per row, else one per workgroup
+  bool by_row;  // a join record per row, else one per workgroup
   int n_waves;
   int g0, gb;    // the group's heads that a launch handles
   float scale;       // 1 / sqrt(head_dim)
