@@ -25,7 +25,11 @@ template <int DT, int NP>
 struct Part {
   uint4 u;
   __device__ __forceinline__ void load(const char* p) { u = ld16(p); }
-  __device__ __forceinline__ void store(char* p) const { st16(p, u); }
+  template <bool STREAM>
+  __device__ __forceinline__ void store(char* p) const {
+    if (STREAM) st16_stream(p, u);
+    else st16(p, u);
+  }
   __device__ __forceinline__ void get(float* f) const {
     if (DT == DT_BF16) {
       unpack16(u, f);
@@ -44,6 +48,7 @@ template <int DT>
 struct Part<DT, 1> {
   uint32_t u;
   __device__ __forceinline__ void load(const char* p) { u = DT == DT_BF16 ? *(const uint16_t*)p : *(const uint32_t*)p; }
+  template <bool>
   __device__ __forceinline__ void store(char* p) const {
     if (DT == DT_BF16) *(uint16_t*)p = (uint16_t)u;
     else *(uint32_t*)p = u;
@@ -65,7 +70,7 @@ __device__ __forceinline__ int problem_of(const int32_t* ends, int P, int t, int
   return lo;
 }
 
-template <int DT, int NP, int D>
+template <int DT, int NP, int D, bool STREAM>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   constexpr int EB = DT == DT_BF16 ? 2 : 4;
   constexpr int LPT = D / (2 * NP), HS = 64 / LPT;  // lanes a head's row is shared by; heads a wave takes at a time
@@ -77,22 +82,48 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   if (t64 >= p.n_tokens) return;
   const int t = (int)t64;
 
+  // The token's rows are asked for first: what is done with them waits for its position, which is up to five memory round trips away (the problem's number,
+  // its offsets, its length, the page).
+  const int slot = lane / LPT, cl = lane % LPT;
+  const bool rotates = cl * NP < p.r / 2;
+  const bool halves = rotates && !p.pairs_layout;
+  // this lane's two parts of a row, NP elements each: x[j..] and x[j + r/2..], or 2 NP consecutive ones
+  const int at0 = (halves ? cl * NP : 2 * cl * NP) * EB, at1 = halves ? at0 + p.r / 2 * EB : at0 + NP * EB;
+  const char* qs = p.q.base ? p.q.base + (int64_t)t * p.q.token : nullptr;
+  const char *ks = p.k.base + (int64_t)t * p.k.token, *vs = p.v.base + (int64_t)t * p.v.token;
+  const int first = qs ? 0 : p.Hq, all = p.Hq + 2 * p.Hkv;
+  const int per = (all - first + (int)gridDim.y * HS - 1) / ((int)gridDim.y * HS) * HS;  // heads of this part of the grid
+  const int h0 = first + blockIdx.y * per;
+  Part<DT, NP> a[U], b[U];
+  auto load = [&](int hb) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = hb + u * HS + slot;
+      if (h < min(all, h0 + per)) {
+        const char* src = h < p.Hq ? qs + h * p.q.head
+                          : h < p.Hq + p.Hkv ? ks + (h - p.Hq) * p.k.head
+                                             : vs + (h - p.Hq - p.Hkv) * p.v.head;
+        a[u].load(src + at0);
+        b[u].load(src + at1);
+      }
+    }
+  };
+  load(h0);
+  const double freq = lane < p.r / 2 ? p.freq[lane] : 0.0;
+
   // the token's problem and place
   int prob = 0, place = 0;
-  bool mine = true, stored = false;
+  bool stored = false;
   if (p.Hkv) {
     int count = 1, i = 0;
     prob = t;
     if (p.offsets) {
       prob = problem_of(p.offsets, p.P, t, lane);
-      mine = prob < p.P && t >= p.offsets[0];
-      if (mine) {
-        const int begin = p.offsets[prob];
-        count = p.offsets[prob + 1] - begin;
-        i = t - begin;
-      }
+      if (prob >= p.P || t < p.offsets[0]) return;  // nobody's row
+      const int begin = p.offsets[prob];
+      count = p.offsets[prob + 1] - begin;
+      i = t - begin;
     }
-    if (!mine) return;
     place = p.lens[prob] - count + i;
     stored = place >= 0 && place < p.capacity;
   }
@@ -106,18 +137,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   // cosines and sines of the token's pairs
   if (lane < p.r / 2) {
     const int pos = p.positions ? p.positions[t] : place;
-    const double turns = (double)pos * (p.freq[lane] * 0.15915494309189533577);  // 1 / (2 pi)
+    const double turns = (double)pos * (freq * 0.15915494309189533577);  // 1 / (2 pi)
     float s, c;
     sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
     turn[wave][lane] = make_float2(p.amplitude * c, p.amplitude * p.sign * s);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-
-  const int slot = lane / LPT, cl = lane % LPT;
-  const bool rotates = cl * NP < p.r / 2;
-  const bool halves = rotates && !p.pairs_layout;
-  // this lane's two parts of a row, NP elements each: x[j..] and x[j + r/2..], or 2 NP consecutive ones
-  const int at0 = (halves ? cl * NP : 2 * cl * NP) * EB, at1 = halves ? at0 + p.r / 2 * EB : at0 + NP * EB;
   float cs[NP], sn[NP];
   if (rotates) {
 #pragma unroll
@@ -128,28 +153,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     }
   }
 
-  const char* qs = p.q.base ? p.q.base + (int64_t)t * p.q.token : nullptr;
   char* qd = p.q_out.base + (int64_t)t * p.q_out.token;
-  const char *ks = p.k.base + (int64_t)t * p.k.token, *vs = p.v.base + (int64_t)t * p.v.token;
   char* kd = p.cache.K + block * p.cache.ks_block + in_block * p.cache.ks_token;
   char* vd = p.cache.V + block * p.cache.vs_block + in_block * p.cache.vs_token;
-  const int first = qs ? 0 : p.Hq, heads = p.Hq + (stored ? 2 * p.Hkv : 0);
-  const int per = ((heads - first + (int)gridDim.y * HS - 1) / ((int)gridDim.y * HS)) * HS;  // heads of this part of the grid
-  const int h0 = first + blockIdx.y * per, h1 = min(heads, h0 + per);
-
-  for (int hb = h0; hb < h1; hb += U * HS) {
-    Part<DT, NP> a[U], b[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = hb + u * HS + slot;
-      if (h < h1) {
-        const char* src = h < p.Hq ? qs + h * p.q.head
-                          : h < p.Hq + p.Hkv ? ks + (h - p.Hq) * p.k.head
-                                             : vs + (h - p.Hq - p.Hkv) * p.v.head;
-        a[u].load(src + at0);
-        b[u].load(src + at1);
-      }
-    }
+  const int h1 = min(stored ? all : p.Hq, h0 + per);
+  for (int hb = h0;;) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int h = hb + u * HS + slot;
@@ -184,21 +192,37 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
       char* dst = h < p.Hq ? qd + h * p.q_out.head
                   : h < p.Hq + p.Hkv ? kd + (h - p.Hq) * p.cache.ks_head
                                      : vd + (h - p.Hq - p.Hkv) * p.cache.vs_head;
-      a[u].store(dst + at0);
-      b[u].store(dst + at1);
+      a[u].template store<STREAM>(dst + at0);
+      b[u].template store<STREAM>(dst + at1);
     }
+    hb += U * HS;
+    if (hb >= h1) break;
+    load(hb);
   }
+}
+
+template <int DT, int NP, bool STREAM>
+void launch_rotary_d(const RotaryParams& p, dim3 grid, hipStream_t s) {
+  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, NP, 128, STREAM>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((rotary_kernel<DT, NP, 64, STREAM>), grid, dim3(256), 0, s, p);
 }
 
 template <int DT, int NP>
 hipError_t launch_rotary_n(const RotaryParams& p, hipStream_t s) {
-  const int HS = 64 / (p.D / (2 * NP));
-  const int rounds = ((p.q.base ? p.Hq : 0) + 2 * p.Hkv + HS - 1) / HS;
+  const int HS = 64 / (p.D / (2 * NP)), heads = (p.q.base ? p.Hq : 0) + 2 * p.Hkv, rounds = (heads + HS - 1) / HS;
   // few tokens: their heads over several waves (latency)
   const int64_t want = (1024 + p.n_tokens - 1) / p.n_tokens;
   const dim3 grid((unsigned)((p.n_tokens + 3) / 4), (unsigned)(want < rounds ? want : rounds));
-  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, NP, 128>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((rotary_kernel<DT, NP, 64>), grid, dim3(256), 0, s, p);
+  // Streaming stores from 48 MB written on: lines that stay in the caches to be written back cost the stream more than they save the next kernel.  us, plain and
+  // streaming, the call alone and with a kernel behind it that reads all it wrote (bf16, 32 + 8 heads of 128 dims): 2048 tokens 12.7 12.0, 36.2 36.5; 4096 25 19, 61.5 63.1; 8192
+  // 47.5 41, 110 114; 32768 158 147, 416 412; 24 prompts of 6532 tokens in all 40.5 28.1; 32767 tokens' queries (28 heads) 91 82.
+  if constexpr (NP > 1) {
+    if (p.n_tokens * heads * p.D * (DT == DT_BF16 ? 2 : 4) >= 48ll << 20) {
+      launch_rotary_d<DT, NP, true>(p, grid, s);
+      return hipGetLastError();
+    }
+  }
+  launch_rotary_d<DT, NP, false>(p, grid, s);
   return hipGetLastError();
 }
 

@@ -7,7 +7,6 @@ current GPU and has the types of the descriptor, since a wrong pointer is not an
 from __future__ import annotations
 
 import ctypes
-import functools
 
 from . import binding
 from .binding import PagedKV, _check, _dtype_of, _stream, lib
@@ -45,8 +44,11 @@ class NewTokens(ctypes.Structure):
                 ("v_stride_token", _i64), ("v_stride_head", _i64), ("q_out_stride_token", _i64), ("q_out_stride_head", _i64)]
 
 
-@functools.lru_cache(maxsize=None)
+_functions = {}
+
+
 def _fn(name):
+    """The library's function, with its argument types."""
     f = getattr(lib(), name)
     f.restype = ctypes.c_size_t if name.endswith("_bytes") else ctypes.c_int
     f.argtypes = {
@@ -56,44 +58,60 @@ def _fn(name):
         "sagekvc_attn_workspace_bytes": [_vp],
         "sagekvc_attn": [_vp] * 6 + [_i32] * 3 + [_vp] * 3 + [ctypes.c_size_t, _vp],
     }[name]
+    _functions[name] = f
     return f
 
 
-@functools.lru_cache(maxsize=None)
-def _element_types():
-    import torch
-
-    return {torch.bfloat16: binding.BF16, torch.float32: binding.F32}, torch.int32
+# The checks below are most of what a call costs on the host (a single token's launch takes 3 us on the GPU and was 8.5 on the host with a function call per
+# tensor and byref per descriptor, 6 as it is).
+_types = {}
 
 
-def _at(t, dtype):
-    """Address of tensor t, which has to have the descriptor's element type and lie on the current GPU; None stays None."""
+def _begin(desc):
+    """(element type of the descriptor, number of the current GPU)."""
+    if not _types:
+        import torch
+
+        device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device) if torch.cuda.is_available() else lambda: None
+        _types.update({binding.BF16: torch.bfloat16, binding.F32: torch.float32, "int": torch.int32, "device": device})
+    return _types[desc.dtype], _types["device"]()
+
+
+def _at(tensors, dtype, device):
+    """Addresses of tensors of one element type on one GPU; None stays None."""
+    got = []
+    for t in tensors:
+        if t is None:
+            got.append(None)
+            continue
+        if t.dtype is not dtype or t.get_device() != device:
+            raise ValueError(f"expected a tensor of {dtype} on GPU {device}, got {t.dtype} on {t.device}")
+        got.append(t.data_ptr())
+    return got
+
+
+def _ints(t, n, device):
+    """Address of an int32 tensor of at least n elements without gaps on that GPU; None stays None."""
     if t is None:
         return None
-    if not t.is_cuda or _element_types()[0].get(t.dtype) != dtype or t.get_device() != _current_device():
-        raise ValueError(f"expected a tensor of the descriptor's element type on the current GPU, got {t.dtype} on {t.device}")
+    if t.dtype is not _types["int"] or t.get_device() != device or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"expected {n} contiguous int32 values on GPU {device}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
-
-
-def _ints(t, n):
-    """Address of an int32 tensor of at least n elements without gaps on the current GPU; None stays None."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.dtype != _element_types()[1] or t.numel() < n or not t.is_contiguous() or t.get_device() != _current_device():
-        raise ValueError(f"expected {n} contiguous int32 values on the current GPU, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr()
-
-
-def _current_device():
-    import torch
-
-    global _current_device
-    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    return _current_device()
 
 
 def _ref(struct):
     return None if struct is None else ctypes.byref(struct)
+
+
+def _place(struct):
+    """Address of a descriptor, kept with it (ctypes.byref makes an object per call)."""
+    if struct is None:
+        return None
+    try:
+        return struct.place
+    except AttributeError:
+        struct.place = ctypes.addressof(struct)
+        return struct.place
 
 
 # ---------------------------------------------------------------------------------------- rotary positions
@@ -140,8 +158,12 @@ def rotary_desc(x, out) -> RotaryDesc:
 
 def sagekvc_rotary(desc: RotaryDesc, rot: RotaryMap, x, positions, out) -> None:
     """out = x's heads rotated by positions (int32 [n]); out may be x."""
-    _check(_fn("sagekvc_rotary")(ctypes.byref(desc), ctypes.byref(rot), _at(x, desc.dtype), _ints(positions, desc.n_tokens),
-                                 _at(out, desc.dtype), _stream()), "sagekvc_rotary")
+    dt, dev = _begin(desc)
+    x, out = _at((x, out), dt, dev)
+    f = _functions.get("sagekvc_rotary") or _fn("sagekvc_rotary")
+    code = f(_place(desc), _place(rot), x, _ints(positions, desc.n_tokens, dev), out, _stream())
+    if code:
+        _check(code, "sagekvc_rotary")
 
 
 # ---------------------------------------------------------------------------------------- the full cache
@@ -192,45 +214,44 @@ def new_tokens(q, k_new, v_new, q_out) -> NewTokens:
         if a[:3] != b[:3] or a[0] != n or a[2] != d or q.dtype != k_new.dtype or q_out.dtype != q.dtype:
             raise ValueError("q and q_out: as many tokens, head_dim and element type as k_new are expected")
         qs = [a[3], a[4], b[3], b[4]]
-    return NewTokens(n, qs[0], qs[1], kt, kh, vs[3], vs[4], qs[2], qs[3])
+    t = NewTokens(n, qs[0], qs[1], kt, kh, vs[3], vs[4], qs[2], qs[3])
+    t.heads = (q.shape[1] if q is not None else 0, hkv)
+    return t
 
 
 def sagekvc_write(desc: CacheDesc, pages, tokens: NewTokens, rot, q, k_new, v_new, token_offsets, seq_lens, positions, q_out, K, V) -> None:
     """New tokens into the cache, keys and queries rotated on the way.  token_offsets int32 [P + 1] or None (one token per problem); seq_lens
     int32 [P], the lengths with the new tokens; positions int32 [n] or None (the places); rot None: no rotation; pages None: dense."""
-    dt, n, P = desc.dtype, tokens.n_tokens, desc.n_problems
-    _heads(q, desc.n_q_heads), _heads(q_out, desc.n_q_heads), _heads(k_new, desc.n_kv_heads), _heads(v_new, desc.n_kv_heads)
-    _check(_fn("sagekvc_write")(ctypes.byref(desc), _ref(pages), ctypes.byref(tokens), _ref(rot), _at(q, dt), _at(k_new, dt), _at(v_new, dt),
-                                _ints(token_offsets, P + 1), _ints(seq_lens, P), _ints(positions, n), _at(q_out, dt), _at(K, dt),
-                                _at(V, dt), _stream()), "sagekvc_write")
-
-
-def _heads(t, n):
-    if t is not None and t.shape[1] != n:
-        raise ValueError(f"{n} heads are expected, got {t.shape[1]}")
+    if tokens.heads != (desc.n_q_heads if q is not None else 0, desc.n_kv_heads):
+        raise ValueError(f"new tokens of {tokens.heads} heads for a cache of {desc.n_q_heads} and {desc.n_kv_heads}")
+    dt, dev = _begin(desc)
+    q, k_new, v_new, q_out, K, V = _at((q, k_new, v_new, q_out, K, V), dt, dev)
+    P = desc.n_problems
+    f = _functions.get("sagekvc_write") or _fn("sagekvc_write")
+    code = f(_place(desc), _place(pages), _place(tokens), _place(rot), q, k_new, v_new, _ints(token_offsets, P + 1, dev), _ints(seq_lens, P, dev),
+             _ints(positions, tokens.n_tokens, dev), q_out, K, V, _stream())
+    if code:
+        _check(code, "sagekvc_write")
 
 
 def sagekvc_attn_workspace_bytes(desc: CacheDesc) -> int:
     return _fn("sagekvc_attn_workspace_bytes")(ctypes.byref(desc))
 
 
-def _floats(t, n):
-    """Address of a float32 tensor of n elements without gaps on the current GPU; None stays None."""
-    if t is None:
-        return None
-    if _at(t, binding.F32) and (t.numel() != n or not t.is_contiguous()):
-        raise ValueError(f"expected {n} contiguous float32 values, got {tuple(t.shape)}")
-    return t.data_ptr()
-
-
 def sagekvc_attn(desc: CacheDesc, pages, q, K, V, seq_lens, max_len: int, n_sink: int, n_recent: int, out, lse, workspace) -> None:
     """Attention of one new token per problem, q [P, Hq, d], over the first seq_lens[p] (int32 [P], at most max_len) tokens of the full cache; n_recent > 0:
     over the first n_sink and the last n_recent of them.  out float32 [P, Hq, d]; lse float32 [P, Hq] or None."""
-    heads = desc.n_problems * desc.n_q_heads
-    if q.numel() != heads * desc.head_dim or not q.is_contiguous():
-        raise ValueError("q: [problems, heads, head_dim], contiguous, is expected")
-    if not workspace.is_cuda or workspace.get_device() != _current_device():
-        raise ValueError("workspace: memory of the current GPU is expected")
-    _check(_fn("sagekvc_attn")(ctypes.byref(desc), _ref(pages), _at(q, desc.dtype), _at(K, desc.dtype), _at(V, desc.dtype),
-                               _ints(seq_lens, desc.n_problems), max_len, n_sink, n_recent, _floats(out, heads * desc.head_dim), _floats(lse, heads),
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "sagekvc_attn")
+    dt, dev = _begin(desc)
+    P, heads = desc.n_problems, desc.n_problems * desc.n_q_heads
+    size = heads * desc.head_dim
+    if q.numel() != size or out.numel() != size or (lse is not None and (lse.numel() != heads or not lse.is_contiguous())) or not (
+            q.is_contiguous() and out.is_contiguous() and workspace.is_contiguous()):
+        raise ValueError("q and out: [problems, heads, head_dim], lse: [problems, heads], contiguous, are expected, and a contiguous workspace")
+    q, K, V = _at((q, K, V), dt, dev)
+    out, lse = _at((out, lse), _types[binding.F32], dev)
+    at, = _at((workspace,), workspace.dtype, dev)
+    f = _functions.get("sagekvc_attn") or _fn("sagekvc_attn")
+    code = f(_place(desc), _place(pages), q, K, V, _ints(seq_lens, P, dev), max_len, n_sink, n_recent, out, lse, at,
+             workspace.numel() * workspace.element_size(), _stream())
+    if code:
+        _check(code, "sagekvc_attn")
