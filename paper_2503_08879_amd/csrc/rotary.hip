@@ -57,18 +57,25 @@ struct Part<DT, 1> {
   __device__ __forceinline__ void set(const float* f) { u = DT == DT_BF16 ? pack_bf16(f[0], 0.f) & 0xFFFFu : __float_as_uint(f[0]); }
 };
 
-// How many of ends[1 .. P] are <= t: the problem that row t belongs to, P past the last.  64 probes at a time, one memory round trip each.
-__device__ __forceinline__ int problem_of(const int32_t* ends, int P, int t, int lane) {
-  int lo = 0, n = P;
-  while (n > 0) {
-    const int step = (n + 63) / 64, k = (lane + 1) * step;
-    const bool below = k <= n && ends[lo + k] <= t;
-    const int m = __popcll(__ballot(below)) * step;
-    lo += m;
-    n = n - m < step - 1 ? n - m : step - 1;
+// How many of ends[1 .. P] are <= t: the problem that row t belongs to, P past the last.  64 probes at a time, one memory round trip each; the first of
+// them is asked for before the rows are, so that it is not waited for behind them.
+struct ProblemSearch {
+  int step, probe;
+  __device__ __forceinline__ void ask(const int32_t* ends, int lo, int n, int lane) {
+    step = (n + 63) / 64;
+    probe = ends[lo + min((lane + 1) * step, n)];
   }
-  return lo;
-}
+  __device__ __forceinline__ int find(const int32_t* ends, int P, int t, int lane) {
+    int lo = 0, n = P;
+    for (;;) {
+      const int m = __popcll(__ballot((lane + 1) * step <= n && probe <= t)) * step;
+      lo += m;
+      n = min(n - m, step - 1);
+      if (n <= 0) return lo;
+      ask(ends, lo, n, lane);
+    }
+  }
+};
 
 template <int DT, int NP, int D, bool STREAM>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
@@ -82,7 +89,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   if (t64 >= p.n_tokens) return;
   const int t = (int)t64;
 
-  // The token's rows are asked for first: what is done with them waits for its position, which is up to five memory round trips away (the problem's number,
+  // The token's rows are asked for early: what is done with them waits for its position, which is up to five memory round trips away (the problem's number,
   // its offsets, its length, the page).
   const int slot = lane / LPT, cl = lane % LPT;
   const bool rotates = cl * NP < p.r / 2;
@@ -108,8 +115,10 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
       }
     }
   };
-  load(h0);
+  ProblemSearch search = {1, 0};
+  if (p.offsets) search.ask(p.offsets, 0, p.P, lane);
   const double freq = lane < p.r / 2 ? p.freq[lane] : 0.0;
+  load(h0);
 
   // the token's problem and place
   int prob = 0, place = 0;
@@ -118,7 +127,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     int count = 1, i = 0;
     prob = t;
     if (p.offsets) {
-      prob = problem_of(p.offsets, p.P, t, lane);
+      prob = search.find(p.offsets, p.P, t, lane);
       if (prob >= p.P || t < p.offsets[0]) return;  // nobody's row
       const int begin = p.offsets[prob];
       count = p.offsets[prob + 1] - begin;
