@@ -186,12 +186,14 @@ struct Mask {
   __device__ __forceinline__ bool cuts(int t0, int n) const { return t0 + n > len || (tail > t0 && t0 + n > S); }
 };
 
+typedef const __attribute__((address_space(1))) char* GlobalBytes;  // (of a plain pointer made from two integers the compiler knows no address space)
+
 // The block that a wave loads next.
 template <int BT>
 struct Ahead : Walk<BT> {
   static constexpr int GPB = BT / 16;  // groups of 16 tokens of a block
   int it;      // block `it` of the part
-  int pages;   // of the next 64 groups, one per lane (a dense cache's "page" is the problem)
+  uint64_t key_at, value_at;  // of the next 64 groups, one per lane: where their tokens begin, in K and in V
   bool valid;  // there is a block
   __device__ __forceinline__ int token0() const { return this->row.token(this->block0 + it); }
   __device__ __forceinline__ void step(const CacheAttnParams& p, int lane) {
@@ -201,35 +203,36 @@ struct Ahead : Walk<BT> {
       it = 0;
     }
     if ((it * GPB & 63) != 0) return;
-    pages = this->prob;
-    if (!p.cache.table) return;
     const int block = min(this->block0 + it + lane / GPB, this->block1 - 1);
-    const int t = min(this->row.token(block) + lane % GPB * 16, this->row.len - 1);
-    const int page = p.cache.table[(int64_t)this->prob * p.cache.pitch + (t >> p.cache.shift)];
-    pages = page < 0 ? 0 : page >= p.cache.n_blocks ? p.cache.n_blocks - 1 : page;
+    const int t = min(this->row.token(block) + lane % GPB * 16, this->row.len - 1), in = t & (int)((1u << p.cache.shift) - 1u);
+    int page = this->prob;  // a dense cache's "page" is the problem
+    if (p.cache.table) {
+      page = p.cache.table[(int64_t)this->prob * p.cache.pitch + (t >> p.cache.shift)];
+      page = page < 0 ? 0 : page >= p.cache.n_blocks ? p.cache.n_blocks - 1 : page;
+    }
+    key_at = (uint64_t)(p.cache.K + this->c * p.cache.ks_head + page * p.cache.ks_block + (int64_t)in * p.cache.ks_token);
+    value_at = (uint64_t)(p.cache.V + this->c * p.cache.vs_head + page * p.cache.vs_block + (int64_t)in * p.cache.vs_token);
   }
   // Group g of the block's groups of 16 tokens, in K or V: where its tokens begin, and how many of them lie behind the first (those behind the row are
   // read as its last one).
   struct Group {
-    const char* at;
+    GlobalBytes at;
     int last;
   };
-  __device__ __forceinline__ Group group(const CacheAttnParams& p, const char* cache, int64_t s_block, int64_t s_head, int s_token, int g) const {
-    const int in_block = (int)((1u << p.cache.shift) - 1u), page = __builtin_amdgcn_readlane(pages, (it * GPB + g) & 63);
-    const int t = min(token0() + 16 * g, this->row.len - 1);
-    return {cache + this->c * s_head + page * s_block + (int64_t)(t & in_block) * s_token, this->row.len - 1 - t};
+  __device__ __forceinline__ Group group(uint64_t at, int g) const {
+    const int k = (it * GPB + g) & 63;
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)at, k), hi = __builtin_amdgcn_readlane((uint32_t)(at >> 32), k);
+    return {(GlobalBytes)((uint64_t)hi << 32 | lo), max(this->row.len - 1 - token0() - 16 * g, 0)};
   }
-  __device__ __forceinline__ Group keys(const CacheAttnParams& p, int g) const {
-    return group(p, p.cache.K, p.cache.ks_block, p.cache.ks_head, p.cache.ks_token, g);
-  }
-  __device__ __forceinline__ Group values(const CacheAttnParams& p, int g) const {
-    return group(p, p.cache.V, p.cache.vs_block, p.cache.vs_head, p.cache.vs_token, g);
-  }
+  __device__ __forceinline__ Group keys(int g) const { return group(key_at, g); }
+  __device__ __forceinline__ Group values(int g) const { return group(value_at, g); }
 };
-// The group's token t of this lane: a wave-uniform address and 32 bits per lane (a token's stride has less than 24).
-template <typename Group>
-__device__ __forceinline__ const char* token_at(const Group& g, int s_token, int t, int offset) {
-  return g.at + (uint32_t)(__umul24((unsigned)min(t, g.last), (unsigned)s_token) + (unsigned)offset);
+// 16 bytes at `offset` of the group's token t of this lane: a wave-uniform address and 32 bits per lane (a token's stride has less than 24).
+template <bool STREAM, typename Group>
+__device__ __forceinline__ uint4 load_token(const Group& g, int s_token, int t, int offset) {
+  const auto* at = (const __attribute__((address_space(1))) u32x4_t*)(g.at + (uint32_t)(__umul24((unsigned)min(t, g.last), (unsigned)s_token) + (unsigned)offset));
+  const u32x4_t v = STREAM ? __builtin_nontemporal_load(at) : *at;
+  return make_uint4(v.x, v.y, v.z, v.w);
 }
 
 // ---- what becomes of a part ----------------------------------------------------------------------
@@ -426,7 +429,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
   constexpr int kSpan = BT * CH;  // 16-byte units
   static_assert(GPAD * D * 4 <= kSpan * 16, "a part's accumulators fit a staging buffer");
   __shared__ uint4 lds[NW][2][kSpan];
-  __shared__ __attribute__((aligned(16))) unsigned short pT[NW][NSET * 16][BT];  // parts of the weights, [part, head][token]
+  __shared__ __attribute__((aligned(16))) unsigned short pT[NW][BT][NSET * 16];  // parts of the weights, [token][part, head]
   __shared__ float2 s_ml[2 * NW][GPAD];
   __shared__ Part s_left[2 * NW];
 
@@ -443,10 +446,12 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
   ahead.step(p, lane);
 
   uint4* buf = lds[wave][1];
+  // rows that no head's parts are in: 2^-126, which adds nothing (0 would make NaN of an infinite value)
 #pragma unroll
-  for (int i = 0; i < NSET * 16 * BT / 512; ++i) reinterpret_cast<uint4*>(&pT[wave][0][0])[i * 64 + lane] = make_uint4(0u, 0u, 0u, 0u);  // rows nobody writes stay 0
+  for (int i = 0; i < NSET * 16 * BT / 512; ++i)
+    reinterpret_cast<uint4*>(&pT[wave][0][0])[i * 64 + lane] = make_uint4(0x00800080u, 0x00800080u, 0x00800080u, 0x00800080u);
   const int hbase = (4 * j) % GPAD, tslot = (4 * j) / GPAD;  // this lane's heads and tile among a q.K accumulator's rows
-  const float cexp = p.scale * 1.44269502162933349609375f;
+  const float cexp = p.scale * 1.44269502162933349609375f, slack = 10.f / cexp;
   auto vswz = [](int t) { return CH == 16 ? (((t & 3) << 1) | (((t >> 3) & 1) << 3)) : ((t & 3) << 1); };
 
   uint4 kv[NLOAD], vv[NLOAD], qa[KSTEPS];
@@ -461,17 +466,17 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
   auto load_k = [&] {
 #pragma unroll
     for (int g = 0; g < BT / 16; ++g) {
-      const auto at = ahead.keys(p, g);
+      const auto at = ahead.keys(g);
 #pragma unroll
-      for (int i = 0; i < 16 / TPL; ++i) kv[g * (16 / TPL) + i] = ld16_stream(token_at(at, p.cache.ks_token, i * TPL + tq, cl * 16));
+      for (int i = 0; i < 16 / TPL; ++i) kv[g * (16 / TPL) + i] = load_token<true>(at, p.cache.ks_token, i * TPL + tq, cl * 16);
     }
   };
   auto load_v = [&] {
 #pragma unroll
     for (int g = 0; g < BT / 16; ++g) {
-      const auto at = ahead.values(p, g);
+      const auto at = ahead.values(g);
 #pragma unroll
-      for (int i = 0; i < 16 / TPL; ++i) vv[g * (16 / TPL) + i] = ld16_stream(token_at(at, p.cache.vs_token, i * TPL + tq, cl * 16));
+      for (int i = 0; i < 16 / TPL; ++i) vv[g * (16 / TPL) + i] = load_token<true>(at, p.cache.vs_token, i * TPL + tq, cl * 16);
     }
   };
   float m_run[4], l_part[4];
@@ -489,7 +494,9 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
     reset();
   }
   while (ahead.valid) {
-    const Part part = {ahead.prob * p.Hkv + ahead.c, ahead.block0, ahead.block1, ahead.row.n, ahead.row_end};
+    const bool last = ahead.block0 + ahead.it + 1 == ahead.block1;  // of the part's blocks
+    Part part;
+    if (last) part = {ahead.prob * p.Hkv + ahead.c, ahead.block0, ahead.block1, ahead.row.n, ahead.row_end};
     const int t0 = ahead.token0();
     const Mask mask(p, ahead.row.len);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the last block's reads of the buffer are done
@@ -506,7 +513,6 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
         if (!mask.at(t0 + i * TPL + tq)) vv[i] = make_uint4(0u, 0u, 0u, 0u);
     }
     ahead.step(p, lane);  // (V of the present block is on its way already)
-    const bool last = !ahead.valid || ahead.it == 0;  // the part's last block
     if (ahead.valid) load_k();
 
     float x[NACC][4];
@@ -530,44 +536,52 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[a][r] = in && hbase + r < gb ? x[a][r] : -INFINITY;
     }
-    // online softmax, once per (token, head), in units of the products; lanes with the same heads agree on the maximum
-    float corr[4];
+    // Online softmax, once per (token, head), in units of the products.  The reference that a head's weights are relative to is raised to its maximum only when
+    // a weight would pass 2^10: what is summed is fp32 with its own exponent, so nothing is lost.  Lanes with the same heads agree on it.
+    bool over = false;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float bm = x[0][r];
+    for (int a = 0; a < NACC; ++a)
 #pragma unroll
-      for (int a = 1; a < NACC; ++a) bm = fmaxf(bm, x[a][r]);
-      bm = group16_max(bm);
-      if (GPAD <= 4) bm = swap16_max(bm);
-      if (GPAD <= 8) bm = swap32_max(bm);
-      const float mn = fmaxf(m_run[r], bm);
-      corr[r] = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[r] - mn) * cexp);
-      float lsum = 0.f;
+      for (int r = 0; r < 4; ++r) over = over || x[a][r] > m_run[r] + slack;
+    if (__ballot(over)) {
 #pragma unroll
-      for (int a = 0; a < NACC; ++a) {
-        const float w = x[a][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[a][r] - mn) * cexp);
-        lsum += w;
-        const int tile = a * TILES + tslot;
-        if (tile < NT) {
-          // three parts of 8 bits; one that is 0 beside a weight that is not becomes bf16's smallest number, so that an infinite value's product
-          // with it is no NaN
-          const uint32_t hi = __float_as_uint(w) & 0xFFFF0000u;
-          const float rest = w - __uint_as_float(hi);
-          uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
-          uint32_t lo = __float_as_uint(rest - __uint_as_float(mid));
-          if (hi != 0u) {
-            mid = mid == 0u ? 0x10000u : mid;
-            lo = (lo >> 16) == 0u ? 0x10000u : lo;
-          }
-          const int col = tile * 16 + n;
-          pT[wave][hbase + r][col] = (unsigned short)(hi >> 16);
-          pT[wave][GPAD + hbase + r][col] = (unsigned short)(mid >> 16);
-          pT[wave][2 * GPAD + hbase + r][col] = (unsigned short)(lo >> 16);
-          if (GPAD == 8) pT[wave][3 * GPAD + hbase + r][col] = hi != 0u;  // beside the lows: no 0 there either
-        }
+      for (int r = 0; r < 4; ++r) {
+        float bm = x[0][r];
+#pragma unroll
+        for (int a = 1; a < NACC; ++a) bm = fmaxf(bm, x[a][r]);
+        bm = group16_max(bm);
+        if (GPAD <= 4) bm = swap16_max(bm);
+        if (GPAD <= 8) bm = swap32_max(bm);
+        const float mn = fmaxf(m_run[r], bm), corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[r] - mn) * cexp);
+        l_part[r] *= corr;
+        m_run[r] = mn;
+#pragma unroll
+        for (int nd = 0; nd < NDT; ++nd) acc[nd][r] *= corr;  // row 4j + r belongs to head hbase + r whatever part it is
       }
-      l_part[r] = l_part[r] * corr[r] + lsum;
-      m_run[r] = mn;
+    }
+#pragma unroll
+    for (int a = 0; a < NACC; ++a) {
+      // A weight in three parts of 8 bits.  None may be 0 where V could be infinite, or their product would be NaN: so the weight's last bit is set and the low
+      // part is kept from vanishing (2^-24 of the weight, and 2^-126).  (V of tokens that are not attended is 0.)
+      uint32_t hi[4], mid[4], lo[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float w = x[a][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[a][r] - m_run[r]) * cexp);
+        l_part[r] += w;
+        const uint32_t u = __float_as_uint(w) | 1u;
+        hi[r] = u & 0xFFFF0000u;
+        const float rest = __uint_as_float(u) - __uint_as_float(hi[r]);
+        mid[r] = __float_as_uint(rest) & 0xFFFF0000u;
+        lo[r] = __float_as_uint(fmaxf(rest - __uint_as_float(mid[r]), 0x1p-126f));
+      }
+      auto pair = [](uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); };  // their upper halves
+      const int tile = a * TILES + tslot;
+      if (tile < NT) {
+        unsigned short* to = &pT[wave][tile * 16 + n][hbase];
+        *reinterpret_cast<uint2*>(to) = make_uint2(pair(hi[0], hi[1]), pair(hi[2], hi[3]));
+        *reinterpret_cast<uint2*>(to + GPAD) = make_uint2(pair(mid[0], mid[1]), pair(mid[2], mid[3]));
+        *reinterpret_cast<uint2*>(to + 2 * GPAD) = make_uint2(pair(lo[0], lo[1]), pair(lo[2], lo[3]));
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // weights visible; q.K's reads of the buffer done
 #pragma unroll
@@ -578,36 +592,32 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (ahead.valid) load_v();
 
-    uint4 pa[BT / 32][NSET];
+    // Transposed reads of LDS: lane s of 16 gives the address of 4 rows (dims) of token s / 4 and receives its own row (dim) of 4 tokens.
+    typedef short v4s_t __attribute__((ext_vector_type(4)));
+    auto transposed = [](const unsigned short* at, const unsigned short* at4) {  // tokens 8 j .. + 3 and the next four
+      const v4s_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s_t*)at);
+      const v4s_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s_t*)at4);
+      struct { v4s_t a, b; } pair = {x0, x1};
+      return __builtin_bit_cast(bf16x8_t, pair);
+    };
+    bf16x8_t pa[BT / 32][NSET];
 #pragma unroll
     for (int kt = 0; kt < BT / 32; ++kt)
 #pragma unroll
-      for (int i = 0; i < NSET; ++i) pa[kt][i] = *reinterpret_cast<const uint4*>(&pT[wave][16 * i + n][32 * kt + 8 * j]);
-    // row 4j + r belongs to head hbase + r whatever part it is
-    if (__ballot(corr[0] != 1.f || corr[1] != 1.f || corr[2] != 1.f || corr[3] != 1.f)) {
-#pragma unroll
-      for (int nd = 0; nd < NDT; ++nd)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[nd][r] *= corr[r];
-    }
+      for (int i = 0; i < NSET; ++i) {
+        const int tu = 32 * kt + 8 * j + (n >> 2), at = 16 * i + (n & 3) * 4;
+        pa[kt][i] = transposed(&pT[wave][tu][at], &pT[wave][tu + 4][at]);
+      }
 #pragma unroll
     for (int nd = 0; nd < NDT; ++nd) {
-      // transposed read: lane s of 16 gives the address of 4 dims of token s / 4 and receives its own dim of 4 tokens
-      typedef short v4s_t __attribute__((ext_vector_type(4)));
       const unsigned short* b16 = reinterpret_cast<const unsigned short*>(buf);
 #pragma unroll
       for (int kt = 0; kt < BT / 32; ++kt) {
         const int tu = 32 * kt + 8 * j + (n >> 2);
         const int cch = (2 * nd + ((n & 3) >> 1)) ^ vswz(tu);  // vswz(tu) = vswz(tu + 4)
-        const v4s_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s_t*)(b16 + (tu * CH + cch) * 8 + (n & 1) * 4));
-        const v4s_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) v4s_t*)(b16 + ((tu + 4) * CH + cch) * 8 + (n & 1) * 4));
-        struct { v4s_t a, b; } pair = {x0, x1};
-        const uint4 vb = __builtin_bit_cast(uint4, pair);
+        const bf16x8_t vb = transposed(b16 + (tu * CH + cch) * 8 + (n & 1) * 4, b16 + ((tu + 4) * CH + cch) * 8 + (n & 1) * 4);
 #pragma unroll
-        for (int i = 0; i < NSET; ++i)
-          acc[nd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, pa[kt][i]), __builtin_bit_cast(bf16x8_t, vb), acc[nd], 0, 0, 0);
+        for (int i = 0; i < NSET; ++i) acc[nd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[kt][i], vb, acc[nd], 0, 0, 0);
       }
     }
 
@@ -630,10 +640,7 @@ __global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnPa
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         float a = acc[nd][r];
-        if (GPAD == 4) {
-          a = j < 3 ? a : 0.f;  // rows 12 to 15 are nobody's: 0 times a value that may be infinite
-          a = swap16_sum(a);
-        }
+        if (GPAD == 4) a = swap16_sum(a);
         if (GPAD <= 8) a = swap32_sum(a);
         acc[nd][r] = a;
       }
@@ -687,14 +694,14 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   auto load_k = [&] {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const char* a = token_at(ahead.keys(p, g / 2), p.cache.ks_token, g % 2 * 8 + t8, sl * 16);
+      const auto at = ahead.keys(g / 2);
 #pragma unroll
-      for (int ch = 0; ch < NC; ++ch) kv[g][ch] = ld16(a + ch * 128);
+      for (int ch = 0; ch < NC; ++ch) kv[g][ch] = load_token<false>(at, p.cache.ks_token, g % 2 * 8 + t8, sl * 16 + ch * 128);
     }
   };
   auto load_v = [&] {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) vv[i] = ld16(token_at(ahead.values(p, i * TPL / 16), p.cache.vs_token, i * TPL % 16 + tq, cl * 16));
+    for (int i = 0; i < NV; ++i) vv[i] = load_token<false>(ahead.values(i * TPL / 16), p.cache.vs_token, i * TPL % 16 + tq, cl * 16);
   };
   constexpr int NQ = (GB * D + 63) / 64;
   float qv[NQ];  // the next part's queries
@@ -727,7 +734,9 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
     keep_q();
   }
   while (ahead.valid) {
-    const Part part = {ahead.prob * p.Hkv + ahead.c, ahead.block0, ahead.block1, ahead.row.n, ahead.row_end};
+    const bool last = ahead.block0 + ahead.it + 1 == ahead.block1;  // of the part's blocks
+    Part part;
+    if (last) part = {ahead.prob * p.Hkv + ahead.c, ahead.block0, ahead.block1, ahead.row.n, ahead.row_end};
     const int t0 = ahead.token0();
     const Mask mask(p, ahead.row.len);
     const bool cut = mask.cuts(t0, BT);
@@ -771,7 +780,6 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
     }
     if (LATE_V) load_v();
     ahead.step(p, lane);
-    const bool last = !ahead.valid || ahead.it == 0;  // the part's last block
     if (ahead.valid) load_k();
 
     // softmax weights, once per (token, head)
