@@ -75,7 +75,7 @@ sagekv_status sagekvc_rotary(const sagekvc_rotary_desc* desc, const sagekvc_rota
 typedef struct {
   int32_t n_problems;       /* sequences                                                          */
   int32_t n_q_heads, n_kv_heads, head_dim, dtype; /* as in sagekv_select_desc; n_q_heads a multiple of n_kv_heads (up to 64 times) */
-  int64_t capacity;         /* tokens a problem has room for; paged: at most table_pitch * page_size */
+  int64_t capacity;         /* tokens a problem has room for, up to 2^30; paged: at most table_pitch * page_size */
   int64_t k_stride_problem; /* elements; *_stride_problem: dense caches only                       */
   int64_t k_stride_head;
   int64_t k_stride_token;
@@ -96,7 +96,7 @@ typedef struct {
 /* Writes new tokens into the cache, keys rotated on the way, and rotates their queries: what stands between a layer's projections and
  * its attention, for prompts (any number of them, of any lengths, whole or in chunks) and for generated tokens alike.
  *   token_offsets  device int32 [n_problems + 1], not decreasing: rows [token_offsets[p], token_offsets[p+1]) are problem p's new tokens, in
- *                  order; a problem may have none.  NULL: one new token per problem, n_tokens = n_problems.
+ *                  order; a problem may have none.  Rows from n_tokens on do not exist.  NULL: one new token per problem, n_tokens = n_problems.
  *   seq_lens       device int32 [n_problems]: the problems' lengths WITH their new tokens (as sagekvc_attn takes them next), so
  *                  the i-th of n_p new tokens gets place seq_lens[p] - n_p + i.
  *   positions      device int32 [n_tokens], the rotation's positions; NULL: the places.
@@ -116,7 +116,7 @@ sagekv_status sagekvc_write(const sagekvc_desc* desc, const sagekv_paged_kv* pag
  * len_p = seq_lens[p] kept within [0, max_len], and, where n_recent > 0, only the tokens t < n_sink and t >= len_p - n_recent (sink and recent
  * window over a cache from which nothing has been evicted).  n_recent = 0 (and n_sink = 0): every token.
  *   q         [n_problems, n_q_heads, head_dim] contiguous;
- *   seq_lens  device int32 [n_problems], read by the launch: one recorded graph serves growing sequences;
+ *   seq_lens  device int32 [n_problems], read by the launch (one recorded graph serves growing sequences), not to be changed while it runs;
  *   max_len   the longest length any problem may have at the launch, 1 <= max_len <= capacity;
  *   out       [n_problems, n_q_heads, head_dim] fp32, contiguous;
  *   lse       nullable, [n_problems, n_q_heads] fp32: log of the sum of exp(logits), with which two parts of a row can be joined.

@@ -81,7 +81,8 @@ sagekv_status check_out(const void* in, int64_t in_token, int64_t in_head, const
 sagekv_status check_cache(const sagekvc_desc* d, const sagekv_paged_kv* pg, const void* K, const void* V, bool written, FullCache* c) {
   if (!d || !K || !V) return SAGEKV_ERR_INVALID_ARG;
   if (d->n_problems < 1 || d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_q_heads % d->n_kv_heads) return SAGEKV_ERR_INVALID_ARG;
-  if (d->capacity < 1 || d->capacity > 0x7FFFFFF0ll) return SAGEKV_ERR_INVALID_ARG;
+  if (d->capacity < 1) return SAGEKV_ERR_INVALID_ARG;
+  if (d->capacity > 1ll << 30) return SAGEKV_ERR_UNSUPPORTED;  // a length and a block beside it stay within 32 bits
   if (check_type(d->dtype, d->head_dim) != SAGEKV_OK) return SAGEKV_ERR_UNSUPPORTED;
   if (d->n_q_heads / d->n_kv_heads > 64 || (int64_t)d->n_problems * d->n_kv_heads > 65535) return SAGEKV_ERR_UNSUPPORTED;
   int64_t k[3] = {d->k_stride_problem, d->k_stride_head, d->k_stride_token};

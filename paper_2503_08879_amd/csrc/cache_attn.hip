@@ -21,8 +21,8 @@ namespace {
 constexpr int NW = 4;  // waves of a workgroup
 
 // ---- rows, weights and shares ------------------------------------------------------------------
-// Lengths do not change while a launch runs: through the constant address space they come by scalar loads, which nothing else waits for.  (A vector
-// load of a length in the middle of a share waits for all of K and V that is in flight.)
+// Lengths do not change while a launch runs (if they do, results are wrong, but no access leaves its buffer): through the constant address space they come
+// by scalar loads, which nothing else waits for.  (A vector load of a length in the middle of a share waits for all of K and V that is in flight.)
 __device__ __forceinline__ int length_of(const CacheAttnParams& p, int prob) {
   return ((const __attribute__((address_space(4))) int*)p.lens)[prob];
 }
@@ -117,7 +117,7 @@ struct Walk {
       }
       // the first lane whose problems reach beyond the share's begin
       const int incl = cuts ? rows * cuts : blocks + rows * kRowWeight;
-      const int hit = __ffsll((unsigned long long)__ballot(before + incl > at)) - 1;
+      const int hit = max(__ffsll((unsigned long long)__ballot(before + incl > at)) - 1, 0);
       before += hit > 0 ? __builtin_amdgcn_readlane(incl, hit - 1) : 0;
       lo += hit * per;
       n = min(per, n - hit * per);
@@ -126,8 +126,8 @@ struct Walk {
       break;
     }
     prob = lo;
-    const int w = weight(), in_problem = at - before;
-    c = in_problem / w;
+    const int w = max(weight(), 1), in_problem = at - before;
+    c = min(in_problem / w, p.Hkv - 1);
     done = in_problem - c * w;
     return shares;
   }
@@ -137,12 +137,14 @@ struct Walk {
   __device__ __forceinline__ bool next(const CacheAttnParams& p) {
     while (at < end) {
       const int w = weight();
-      if (done == w) {
+      if (done >= w) {
         done = 0;
         if (++c == p.Hkv) {
           c = 0;
-          do row = RowBlocks<BT>(p, length_of(p, ++prob));
-          while (row.n == 0 && prob + 1 < p.P);
+          do {
+            if (++prob == p.P) return false;
+            row = RowBlocks<BT>(p, length_of(p, prob));
+          } while (row.n == 0);
         }
         continue;
       }

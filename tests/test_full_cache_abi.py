@@ -147,7 +147,7 @@ def cache_args(paged=True, **change):
 
 CACHE_REFUSALS = [
     (INVALID, True, dict(n_problems=0)), (INVALID, True, dict(n_kv_heads=3)), (INVALID, True, dict(n_kv_heads=0)),
-    (INVALID, True, dict(capacity=0)), (INVALID, False, dict(capacity=0x7FFFFFF1)), (UNSUPPORTED, True, dict(head_dim=32)),
+    (INVALID, True, dict(capacity=0)), (UNSUPPORTED, False, dict(capacity=(1 << 30) + 1)), (UNSUPPORTED, True, dict(head_dim=32)),
     (UNSUPPORTED, True, dict(dtype=7)), (UNSUPPORTED, True, dict(n_q_heads=130)), (UNSUPPORTED, True, dict(n_problems=40000)),
     (INVALID, True, dict(block_table=None)), (UNSUPPORTED, True, dict(block_table=P16 + 2)), (INVALID, True, dict(n_pages=0)),
     (INVALID, True, dict(page_size=8)), (INVALID, True, dict(page_size=48)), (INVALID, True, dict(table_pitch=6)),
@@ -205,11 +205,11 @@ def test_attn_refusals(code, paged, change):
 
 
 def test_attn_of_more_work_than_can_be_numbered():
-    """65535 rows of 2^31 tokens, all through strides of 0: more than 2^31 steps."""
-    desc = sk.CacheDesc(65535, 1, 1, 64, sk.BF16, 0x7FFFFFF0, 0, 0, 64, 0, 0, 64)
+    """65535 rows of 2^30 tokens, all through strides of 0: more than 2^31 blocks."""
+    desc = sk.CacheDesc(65535, 1, 1, 64, sk.BF16, 1 << 30, 0, 0, 64, 0, 0, 64)
     f = fc._fn("sagekvc_attn")
     size = sk.sagekvc_attn_workspace_bytes(desc)
-    assert f(byref(desc), None, P16, P16, P16, P16, 0x7FFFFFF0, 0, 0, P16, None, P16, size, None) == UNSUPPORTED
+    assert f(byref(desc), None, P16, P16, P16, P16, 1 << 30, 0, 0, P16, None, P16, size, None) == UNSUPPORTED
 
 
 def test_attn_workspace():
