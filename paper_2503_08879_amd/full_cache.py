@@ -104,14 +104,8 @@ def _ref(struct):
 
 
 def _place(struct):
-    """Address of a descriptor, kept with it (ctypes.byref makes an object per call)."""
-    if struct is None:
-        return None
-    try:
-        return struct.place
-    except AttributeError:
-        struct.place = ctypes.addressof(struct)
-        return struct.place
+    """Address of a descriptor (ctypes.byref makes an object per call)."""
+    return None if struct is None else ctypes.addressof(struct)
 
 
 # ---------------------------------------------------------------------------------------- rotary positions
@@ -222,8 +216,9 @@ def new_tokens(q, k_new, v_new, q_out) -> NewTokens:
 def sagekvc_write(desc: CacheDesc, pages, tokens: NewTokens, rot, q, k_new, v_new, token_offsets, seq_lens, positions, q_out, K, V) -> None:
     """New tokens into the cache, keys and queries rotated on the way.  token_offsets int32 [P + 1] or None (one token per problem); seq_lens
     int32 [P], the lengths with the new tokens; positions int32 [n] or None (the places); rot None: no rotation; pages None: dense."""
-    if tokens.heads != (desc.n_q_heads if q is not None else 0, desc.n_kv_heads):
-        raise ValueError(f"new tokens of {tokens.heads} heads for a cache of {desc.n_q_heads} and {desc.n_kv_heads}")
+    heads = getattr(tokens, "heads", None)  # (strides filled in by hand know of none)
+    if heads is not None and heads != (desc.n_q_heads if q is not None else 0, desc.n_kv_heads):
+        raise ValueError(f"new tokens of {heads} heads for a cache of {desc.n_q_heads} and {desc.n_kv_heads}")
     dt, dev = _begin(desc)
     q, k_new, v_new, q_out, K, V = _at((q, k_new, v_new, q_out, K, V), dt, dev)
     P = desc.n_problems

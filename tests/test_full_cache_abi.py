@@ -1,4 +1,5 @@
 """The calls on the full cache without a GPU: declarations, descriptor sizes, refusals (nothing is launched), frequencies."""
+import copy
 import ctypes
 import math
 import os
@@ -234,3 +235,13 @@ def test_descriptor_makers_refuse_tensors_they_cannot_describe():
     desc = sk.rotary_desc(x, x)
     with pytest.raises(ValueError):  # host memory
         sk.sagekvc_rotary(desc, sk.RotaryMap(128, 0, 0, 1.0, P16), x, torch.zeros(4, dtype=torch.int32), x)
+
+
+def test_a_copied_descriptor_stands_for_itself():
+    """A call takes the fields of the descriptor it is given, also where that is a changed copy of one that was used before."""
+    desc = sk.CacheDesc(3, 8, 2, 128, sk.BF16, 100, 0, 0, 0, 0, 0, 0)
+    fc._place(desc)
+    other = copy.copy(desc)
+    other.n_problems = 2
+    seen = sk.CacheDesc.from_address(fc._place(other))
+    assert seen.n_problems == 2 and sk.CacheDesc.from_address(fc._place(desc)).n_problems == 3
