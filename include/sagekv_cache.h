@@ -73,7 +73,7 @@ sagekv_status sagekvc_rotary(const sagekvc_rotary_desc* desc, const sagekvc_rota
 
 /* ---- the full cache ----------------------------------------------------------------------------- */
 typedef struct {
-  int32_t n_problems;       /* sequences                                                          */
+  int32_t n_problems;       /* sequences; n_problems * n_kv_heads <= 65535                        */
   int32_t n_q_heads, n_kv_heads, head_dim, dtype; /* as in sagekv_select_desc; n_q_heads a multiple of n_kv_heads (up to 64 times) */
   int64_t capacity;         /* tokens a problem has room for, up to 2^30; paged: at most table_pitch * page_size */
   int64_t k_stride_problem; /* elements; *_stride_problem: dense caches only                       */

@@ -328,7 +328,8 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
   __shared__ float s_max[4];
   __shared__ double s_den[4];
   const JoinRecord r = p.joins[blockIdx.x];
-  if (r.first < 0) return;
+  // (the bounds are for lengths that changed under the call: a record that nobody wrote is whatever the workspace held)
+  if (r.first < 0 || r.last < r.first || r.last >= kAttnGroups || (unsigned)r.row >= (unsigned)(p.P * p.Hkv)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = r.last - r.first + 1;
   const float c = p.join_scale * 1.44269502162933349609375f;
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
 // cost one product as they would with weights rounded to bf16, eight two, sixteen three.  (Rounded to bf16 the weights would put the outputs 1e-3 off, fp32's
 // own error is 1e-6, and the matrix cores have nothing else to do: four blocks of 128 dims are 64 KB, 2.5 us of HBM time for a CU.)
 template <int D, int GPAD>
-__global__ __launch_bounds__(NW * 64, 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
+__global__ __launch_bounds__(NW * 64, D == 64 && GPAD > 4 ? 1 : 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
   constexpr int BT = attn_block(DT_BF16, D);
   constexpr int CH = D / 8, TPL = 64 / CH, NLOAD = BT / TPL, KSTEPS = D / 32;
   constexpr int TILES = 16 / GPAD, NT = BT / 16;     // tiles of 16 tokens a q.K accumulator has slots for, tiles of a block

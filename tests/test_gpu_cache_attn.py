@@ -138,6 +138,35 @@ def test_many_problems(P):
     case([500] + [0] * (P - 1), 4, 2, 64, "float32", dense=True, check={0, 1, P - 1})
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("P", [32, 70, 200, 450, 1100])
+def test_short_rows_shared_out_whole(dtype, P):
+    """Rows of a few blocks, all of them and those of a window: four waves, two or one per row, several rows per wave; a few empty ones."""
+    rng = np.random.default_rng(P)
+    lens = [int(x) * int(x > 5) for x in rng.integers(0, 97, P)]
+    lens[P // 2] = 97
+    check = set(int(x) for x in rng.integers(0, P, 60)) | {0, P // 2, P - 1}
+    case(lens, 6, 2, 128, dtype, check=check, seed=1)
+    case(lens, 6, 2, 64, dtype, True, S=3, W=50, check=check, seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_many_rows_of_groups_that_take_several_launches(dtype):
+    rng = np.random.default_rng(20)
+    lens = [int(np.exp(rng.uniform(0, np.log(900)))) for _ in range(300)]
+    lens[7], lens[8], lens[299] = 0, 900, 899
+    check = set(int(x) for x in rng.integers(0, 300, 40)) | {6, 7, 8, 9, 299}
+    case(lens, 40, 2, 64, dtype, check=check)
+
+
+def test_as_many_rows_as_a_call_takes():
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in rng.integers(0, 17, 65535)]
+    lens[65534] = 16
+    check = set(int(x) for x in rng.integers(0, 65535, 300)) | {0, 65534}
+    case(lens, 2, 1, 64, dense=True, poison=False, check=check)
+
+
 def test_nothing_to_attend_anywhere():
     case([0, 0, 0], 4, 2, 128, cap=300)
     case([0], 4, 2, 64, "float32", dense=True, cap=1)
