@@ -1,6 +1,7 @@
 // Attention of one new token per sequence over the full cache, every sequence of its own length.
 //
-// A row (sequence, KV head) is cut into blocks of 32 tokens (fp32, 128 dims: 16), a wave's work at a time.  All rows, one after the other, are divided
+// A row (sequence, KV head) is cut into blocks of 16 KB of K and V (bf16, 128 dims: 32 tokens), a wave's work at a time.  (Blocks of twice that at 128 dims: one
+// sequence of 512K tokens 325 us instead of 318, and short rows end in larger remainders.)  All rows, one after the other, are divided
 // over the launch's waves, whatever their lengths: a row weighs its blocks and kRowWeight more for its beginning and end, and every wave gets the same
 // weight, a run of blocks that may hold several rows and two parts of rows at most, one that continues a row and one that begins
 // one.  A wave finds its share from the lengths alone, which it reads on the device (64 of them at a time, summed over the wave), and goes through it without waiting for
@@ -8,9 +9,11 @@
 // four waves of the workgroup, whose shares are neighbours, are done, and are merged there, (max, sum, accumulator) by (max, sum, accumulator).  What the
 // workgroup then has not got the whole of goes to scratch, one row that it continues and one that it begins at most, and join_kernel merges that.
 // (With shares for workgroups, whose four waves took a row's blocks in turn and merged them at its end, a row cost as much as 8 blocks, and 64 sequences of
-// 1 to 32K tokens 88 us.)
+// 1 to 32K tokens 88 us instead of 80.)
 //
-// Bound by HBM: K and V are read once, for all heads of the group at a time.
+// One workgroup per CU.  (With two, the older one of a CU and some XCDs get ahead: one sequence of 512K tokens ends its loop between 267 and 321 us, with one between 294
+// and 308.)  Bound by HBM: K and V are read once, for all heads of the group at a time.  Short calls are bound by latency: lengths, pages, the first block and the
+// join come one after the other, 6.5 us of a call, and a block takes a wave 1.35 us (fp32 1.8) however little the others read.
 #include "device_utils.h"
 #include "full_cache.h"
 
@@ -414,12 +417,15 @@ __global__ __launch_bounds__(256) void join_kernel(CacheAttnParams p) {
   }
 }
 
-// bf16 caches.  A wave takes 32 tokens at a time: K goes through the wave's staging buffer in LDS (16-byte chunks, XOR-swizzled) into
+// bf16 caches.  A block of a wave: K goes through the wave's staging buffer in LDS (16-byte chunks, XOR-swizzled) into
 // v_mfma_f32_16x16x32_bf16 with the queries as the A operand, their rows repeated, so that a lane takes the tile of its slot and ends
 // with 4 logits of one token; V goes through the same buffer and is read transposed (ds_read_b64_tr_b16).  A softmax weight, fp32, is cut into three bf16
 // parts of 8 bits each, which add up to it exactly: rows of the second product's A operand that the group's heads leave free take them, so up to four heads
 // cost one product as they would with weights rounded to bf16, eight two, sixteen three.  (Rounded to bf16 the weights would put the outputs 1e-3 off, fp32's
-// own error is 1e-6, and the matrix cores have nothing else to do: four blocks of 128 dims are 64 KB, 2.5 us of HBM time for a CU.)
+// own error is 1e-6, and the matrix cores have nothing else to do: a workgroup's four blocks are 64 KB, which the CU's share of HBM brings in 2.4 us.)
+//
+// 8 rows of 524301 tokens, 4 heads, 128 dims: 321 us, 6.7 TB/s (7.1 to 7.4 is what reads alone reach); 256 rows of 1 to 32K tokens, 7 heads: 80 us, 5.2 TB/s; 8 rows of 32001: 30
+// us, 4.4 TB/s.
 template <int D, int GPAD>
 __global__ __launch_bounds__(NW * 64, D == 64 && GPAD > 4 ? 1 : 2) void cache_attn_bf16_kernel(CacheAttnParams p) {
   constexpr int BT = attn_block(DT_BF16, D);

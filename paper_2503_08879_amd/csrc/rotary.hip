@@ -2,9 +2,15 @@
 //
 // A wave takes one token: its position, its place and the page's table entry are wave-uniform, and lane j forms pair j's angle
 // (at most 64 pairs), pos * f in turns, reduced in fp64 to [-1/2, 1/2], its cosine and sine in fp32.  They go through LDS to the lanes that need
-// them, once per token for all heads.  Then a head's row is shared by the lanes in steps of 2 NP elements: NP pairs, or 2 NP elements
-// to copy; 16-byte loads and stores where rotary_dim allows it (NP = 8 bf16, 4 fp32), single elements (NP = 1) where it
-// does not.  Bound by HBM (prompts: every element read and written once) or by latency (single tokens).
+// them, once per token for all heads.  Then a head's row is shared by its lanes in two 16-byte parts each, one in
+// each half of the row, neighbouring lanes' parts side by side for every load and store.  Where a pair's other member is, is the MODE:
+//   HALVES  pairs (j, j + d/2) of whole rows: both members with one lane (rows that are only copied come here too);
+//   PAIRS   pairs (2j, 2j + 1), r any: a part is whole pairs;
+//   APART   pairs (j, j + r/2), r < d: a lane's elements find their other members in the row's copy in LDS.
+// (us: two consecutive parts per lane in PAIRS 105 instead of 84, for 32767 tokens of 28 heads of 128 dims, bf16; a pair's members with one lane where r = 64, so that
+// loads and stores are in pieces of 64 bytes, 93 instead of 89; single elements instead of parts where r = 20, for a prompt of 131072 tokens, 32 + 8 heads, 1009 instead of 579.)
+//
+// Bound by HBM (prompts: every element read and written once) or by latency (single tokens).
 #include "device_utils.h"
 #include "full_cache.h"
 
@@ -20,9 +26,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
 }
 
-// NP consecutive elements of a row in registers, as they are in memory.
-template <int DT, int NP>
+enum { HALVES, PAIRS, APART };
+
+// 16 bytes of a row in registers, as they are in memory: N elements.
+template <int DT>
 struct Part {
+  static constexpr int N = DT == DT_BF16 ? 8 : 4;
   uint4 u;
   __device__ __forceinline__ void load(const char* p) { u = ld16(p); }
   template <bool STREAM>
@@ -43,18 +52,16 @@ struct Part {
     else
       u = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
-};
-template <int DT>
-struct Part<DT, 1> {
-  uint32_t u;
-  __device__ __forceinline__ void load(const char* p) { u = DT == DT_BF16 ? *(const uint16_t*)p : *(const uint32_t*)p; }
-  template <bool>
-  __device__ __forceinline__ void store(char* p) const {
-    if (DT == DT_BF16) *(uint16_t*)p = (uint16_t)u;
-    else *(uint32_t*)p = u;
+  // the first n elements (an even number) set, the others as they are
+  __device__ __forceinline__ void set_first(const float* f, int n) {
+    const uint4 old = u;
+    constexpr int E = DT == DT_BF16 ? 2 : 1;  // elements of 4 bytes
+    set(f);
+    u.x = n > 0 ? u.x : old.x;
+    u.y = n > E ? u.y : old.y;
+    u.z = n > 2 * E ? u.z : old.z;
+    u.w = n > 3 * E ? u.w : old.w;
   }
-  __device__ __forceinline__ void get(float* f) const { f[0] = __uint_as_float(DT == DT_BF16 ? u << 16 : u); }
-  __device__ __forceinline__ void set(const float* f) { u = DT == DT_BF16 ? pack_bf16(f[0], 0.f) & 0xFFFFu : __float_as_uint(f[0]); }
 };
 
 // How many of ends[1 .. P] are <= t: the problem that row t belongs to, P past the last.  64 probes at a time, one memory round trip each; the first of
@@ -77,12 +84,13 @@ struct ProblemSearch {
   }
 };
 
-template <int DT, int NP, int D, bool STREAM>
+template <int DT, int MODE, int D, bool STREAM>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
-  constexpr int EB = DT == DT_BF16 ? 2 : 4;
+  constexpr int EB = DT == DT_BF16 ? 2 : 4, NP = Part<DT>::N;
   constexpr int LPT = D / (2 * NP), HS = 64 / LPT;  // lanes a head's row is shared by; heads a wave takes at a time
-  constexpr int U = NP == 1 ? 8 : 4;                // rounds of heads in flight
+  constexpr int U = 4;                              // rounds of heads in flight
   __shared__ float2 turn[4][64];
+  __shared__ uint4 copy[MODE == APART ? 4 : 1][MODE == APART ? 128 : 1];  // APART: a wave's rows
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t64 = (int64_t)blockIdx.x * 4 + wave;
@@ -92,16 +100,15 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   // The token's rows are asked for early: what is done with them waits for its position, which is up to five memory round trips away (the problem's number,
   // its offsets, its length, the page).
   const int slot = lane / LPT, cl = lane % LPT;
-  const bool rotates = cl * NP < p.r / 2;
-  const bool halves = rotates && !p.pairs_layout;
-  // this lane's two parts of a row, NP elements each: x[j..] and x[j + r/2..], or 2 NP consecutive ones
-  const int at0 = (halves ? cl * NP : 2 * cl * NP) * EB, at1 = halves ? at0 + p.r / 2 * EB : at0 + NP * EB;
+  const bool rotates = cl * NP < p.r;
+  const int e0 = cl * NP, e1 = D / 2 + e0, half = p.r / 2;  // first elements of this lane's two parts of a row
+  const int at0 = e0 * EB, at1 = e1 * EB;
   const char* qs = p.q.base ? p.q.base + (int64_t)t * p.q.token : nullptr;
   const char *ks = p.k.base + (int64_t)t * p.k.token, *vs = p.v.base + (int64_t)t * p.v.token;
   const int first = qs ? 0 : p.Hq, all = p.Hq + 2 * p.Hkv;
   const int per = (all - first + (int)gridDim.y * HS - 1) / ((int)gridDim.y * HS) * HS;  // heads of this part of the grid
   const int h0 = first + blockIdx.y * per;
-  Part<DT, NP> a[U], b[U];
+  Part<DT> a[U], b[U];
   auto load = [&](int hb) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -152,13 +159,17 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     turn[wave][lane] = make_float2(p.amplitude * c, p.amplitude * p.sign * s);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  float cs[NP], sn[NP];
+  // HALVES: of the pairs that both parts share; PAIRS: of the first part's, then the second's; APART: of the elements, sines with their signs
+  constexpr int NC = MODE == APART ? 2 * NP : NP;
+  float cs[NC], sn[NC];
   if (rotates) {
 #pragma unroll
-    for (int e = 0; e < NP; ++e) {
-      const float2 v = turn[wave][cl * NP + e];
-      cs[e] = v.x;
-      sn[e] = v.y;
+    for (int i = 0; i < NC; ++i) {
+      const int e = MODE == HALVES ? 0 : i < NC / 2 ? e0 : e1, k = i % (NC / 2);
+      const int j = MODE == HALVES ? e0 + i : MODE == PAIRS ? e / 2 + k : e + k < half ? e + k : e + k - half;
+      const float2 v = turn[wave][min(j, 63)];  // (behind the last pair: not used)
+      cs[i] = v.x;
+      sn[i] = MODE == APART && e + k < half ? -v.y : v.y;
     }
   }
 
@@ -172,30 +183,40 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
       const int h = hb + u * HS + slot;
       if (h >= h1) continue;
       if (rotates && h < p.Hq + p.Hkv) {
-        float x[NP], y[NP];
-        a[u].get(x);
-        b[u].get(y);
-        if (NP > 1 && p.pairs_layout) {  // 2 NP consecutive elements: x, y hold the pairs' members in turn
-          float z[2 * NP];
-#pragma unroll
-          for (int e = 0; e < NP; ++e) z[e] = x[e], z[NP + e] = y[e];
+        float x[2][NP], y[2][NP];
+        a[u].get(x[0]);
+        b[u].get(x[1]);
+        if (MODE == HALVES) {
 #pragma unroll
           for (int e = 0; e < NP; ++e) {
-            const float xe = z[2 * e] * cs[e] - z[2 * e + 1] * sn[e], ye = z[2 * e + 1] * cs[e] + z[2 * e] * sn[e];
-            z[2 * e] = xe;
-            z[2 * e + 1] = ye;
+            y[0][e] = x[0][e] * cs[e] - x[1][e] * sn[e];
+            y[1][e] = x[1][e] * cs[e] + x[0][e] * sn[e];
           }
-          a[u].set(z);
-          b[u].set(z + NP);
+          a[u].set(y[0]);
+          b[u].set(y[1]);
+        } else if (MODE == PAIRS) {
+#pragma unroll
+          for (int e = 0; e < 2 * NP; e += 2) {
+            const float m = x[e / NP][e % NP], n = x[e / NP][e % NP + 1], c = cs[e / 2], s = sn[e / 2];
+            y[e / NP][e % NP] = m * c - n * s;
+            y[e / NP][e % NP + 1] = n * c + m * s;
+          }
+          a[u].set_first(y[0], p.r - e0);
+          b[u].set_first(y[1], p.r - e1);
         } else {
+          char* row = (char*)copy[wave] + slot * (D * EB);
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          *(uint4*)(row + at0) = a[u].u;
+          *(uint4*)(row + at1) = b[u].u;
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-          for (int e = 0; e < NP; ++e) {
-            const float xe = x[e] * cs[e] - y[e] * sn[e], ye = y[e] * cs[e] + x[e] * sn[e];
-            x[e] = xe;
-            y[e] = ye;
+          for (int i = 0; i < 2 * NP; ++i) {
+            const int e = (i < NP ? e0 : e1) + i % NP, o = e < half ? e + half : e - half;  // o < D also where e >= r
+            const float other = DT == DT_BF16 ? __uint_as_float((uint32_t)((const uint16_t*)row)[o] << 16) : ((const float*)row)[o];
+            y[i / NP][i % NP] = x[i / NP][i % NP] * cs[i] + other * sn[i];
           }
-          a[u].set(x);
-          b[u].set(y);
+          a[u].set_first(y[0], p.r - e0);
+          b[u].set_first(y[1], p.r - e1);
         }
       }
       char* dst = h < p.Hq ? qd + h * p.q_out.head
@@ -210,37 +231,36 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   }
 }
 
-template <int DT, int NP, bool STREAM>
+template <int DT, int MODE, bool STREAM>
 void launch_rotary_d(const RotaryParams& p, dim3 grid, hipStream_t s) {
-  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, NP, 128, STREAM>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((rotary_kernel<DT, NP, 64, STREAM>), grid, dim3(256), 0, s, p);
+  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128, STREAM>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, STREAM>), grid, dim3(256), 0, s, p);
 }
 
-template <int DT, int NP>
-hipError_t launch_rotary_n(const RotaryParams& p, hipStream_t s) {
-  const int HS = 64 / (p.D / (2 * NP)), heads = (p.q.base ? p.Hq : 0) + 2 * p.Hkv, rounds = (heads + HS - 1) / HS;
+template <int DT, int MODE>
+hipError_t launch_rotary_m(const RotaryParams& p, hipStream_t s) {
+  const int HS = 64 / (p.D / (2 * Part<DT>::N)), heads = (p.q.base ? p.Hq : 0) + 2 * p.Hkv, rounds = (heads + HS - 1) / HS;
   // few tokens: their heads over several waves (latency)
   const int64_t want = (1024 + p.n_tokens - 1) / p.n_tokens;
   const dim3 grid((unsigned)((p.n_tokens + 3) / 4), (unsigned)(want < rounds ? want : rounds));
   // Streaming stores from 48 MB written on: lines that stay in the caches to be written back cost the stream more than they save the next kernel.  us, plain and
   // streaming, the call alone and with a kernel behind it that reads all it wrote (bf16, 32 + 8 heads of 128 dims): 2048 tokens 12.7 12.0, 36.2 36.5; 4096 25 19, 61.5 63.1; 8192
   // 47.5 41, 110 114; 32768 158 147, 416 412; 24 prompts of 6532 tokens in all 40.5 28.1; 32767 tokens' queries (28 heads) 91 82.
-  if constexpr (NP > 1) {
-    if (p.n_tokens * heads * p.D * (DT == DT_BF16 ? 2 : 4) >= 48ll << 20) {
-      launch_rotary_d<DT, NP, true>(p, grid, s);
-      return hipGetLastError();
-    }
-  }
-  launch_rotary_d<DT, NP, false>(p, grid, s);
+  if (p.n_tokens * heads * p.D * (DT == DT_BF16 ? 2 : 4) >= 48ll << 20) launch_rotary_d<DT, MODE, true>(p, grid, s);
+  else launch_rotary_d<DT, MODE, false>(p, grid, s);
   return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_rotary_t(const RotaryParams& p, hipStream_t s) {
+  if (p.r && p.pairs_layout) return launch_rotary_m<DT, PAIRS>(p, s);
+  return p.r == 0 || p.r == p.D ? launch_rotary_m<DT, HALVES>(p, s) : launch_rotary_m<DT, APART>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_rotary(const RotaryParams& p, hipStream_t s) {
-  // 16-byte parts: a half, or the rotated elements, have to end at a part's end
-  if (p.dtype == DT_BF16) return p.r % 16 == 0 ? launch_rotary_n<DT_BF16, 8>(p, s) : launch_rotary_n<DT_BF16, 1>(p, s);
-  return p.r % 8 == 0 ? launch_rotary_n<DT_F32, 4>(p, s) : launch_rotary_n<DT_F32, 1>(p, s);
+  return p.dtype == DT_BF16 ? launch_rotary_t<DT_BF16>(p, s) : launch_rotary_t<DT_F32>(p, s);
 }
 
 }  // namespace sagekv
