@@ -10,6 +10,10 @@
 // (us: two consecutive parts per lane in PAIRS 105 instead of 84, for 32767 tokens of 28 heads of 128 dims, bf16; a pair's members with one lane where r = 64, so that
 // loads and stores are in pieces of 64 bytes, 93 instead of 89; single elements instead of parts where r = 20, for a prompt of 131072 tokens, 32 + 8 heads, 1009 instead of 579.)
 //
+// Stores are streaming ones: what stays in the caches has to be written back when the kernel ends, which nothing overlaps.  us, plain and streaming, 32 heads of 128
+// dims, bf16: 512 tokens 5.5 5.3, 2048 10.5 7.3, 4096 14.0 13.8, 8192 29.0 28.3; with a kernel behind it that reads all that was written 10.1 10.1, 16.8 16.9, 27.0 25.9, 52.1 50.4; 24
+// prompts of 6532 tokens in all, with their keys and values, 38.1 25.9; a layer's write and attention of one token each of 64 sequences the same.
+//
 // Bound by HBM (prompts: every element read and written once) or by latency (single tokens).
 #include "device_utils.h"
 #include "full_cache.h"
@@ -34,11 +38,7 @@ struct Part {
   static constexpr int N = DT == DT_BF16 ? 8 : 4;
   uint4 u;
   __device__ __forceinline__ void load(const char* p) { u = ld16(p); }
-  template <bool STREAM>
-  __device__ __forceinline__ void store(char* p) const {
-    if (STREAM) st16_stream(p, u);
-    else st16(p, u);
-  }
+  __device__ __forceinline__ void store(char* p) const { st16_stream(p, u); }
   __device__ __forceinline__ void get(float* f) const {
     if (DT == DT_BF16) {
       unpack16(u, f);
@@ -84,7 +84,7 @@ struct ProblemSearch {
   }
 };
 
-template <int DT, int MODE, int D, bool STREAM>
+template <int DT, int MODE, int D>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   constexpr int EB = DT == DT_BF16 ? 2 : 4, NP = Part<DT>::N;
   constexpr int LPT = D / (2 * NP), HS = 64 / LPT;  // lanes a head's row is shared by; heads a wave takes at a time
@@ -222,19 +222,13 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
       char* dst = h < p.Hq ? qd + h * p.q_out.head
                   : h < p.Hq + p.Hkv ? kd + (h - p.Hq) * p.cache.ks_head
                                      : vd + (h - p.Hq - p.Hkv) * p.cache.vs_head;
-      a[u].template store<STREAM>(dst + at0);
-      b[u].template store<STREAM>(dst + at1);
+      a[u].store(dst + at0);
+      b[u].store(dst + at1);
     }
     hb += U * HS;
     if (hb >= h1) break;
     load(hb);
   }
-}
-
-template <int DT, int MODE, bool STREAM>
-void launch_rotary_d(const RotaryParams& p, dim3 grid, hipStream_t s) {
-  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128, STREAM>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, STREAM>), grid, dim3(256), 0, s, p);
 }
 
 template <int DT, int MODE>
@@ -243,11 +237,8 @@ hipError_t launch_rotary_m(const RotaryParams& p, hipStream_t s) {
   // few tokens: their heads over several waves (latency)
   const int64_t want = (1024 + p.n_tokens - 1) / p.n_tokens;
   const dim3 grid((unsigned)((p.n_tokens + 3) / 4), (unsigned)(want < rounds ? want : rounds));
-  // Streaming stores from 48 MB written on: lines that stay in the caches to be written back cost the stream more than they save the next kernel.  us, plain and
-  // streaming, the call alone and with a kernel behind it that reads all it wrote (bf16, 32 + 8 heads of 128 dims): 2048 tokens 12.7 12.0, 36.2 36.5; 4096 25 19, 61.5 63.1; 8192
-  // 47.5 41, 110 114; 32768 158 147, 416 412; 24 prompts of 6532 tokens in all 40.5 28.1; 32767 tokens' queries (28 heads) 91 82.
-  if (p.n_tokens * heads * p.D * (DT == DT_BF16 ? 2 : 4) >= 48ll << 20) launch_rotary_d<DT, MODE, true>(p, grid, s);
-  else launch_rotary_d<DT, MODE, false>(p, grid, s);
+  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
