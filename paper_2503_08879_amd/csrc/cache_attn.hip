@@ -12,7 +12,7 @@
 // 1 to 32K tokens 88 us instead of 80.)
 //
 // One workgroup per CU.  (With two, the older one of a CU and some XCDs get ahead: one sequence of 512K tokens ends its loop between 267 and 321 us, with one between 294
-// and 308.)  Bound by HBM: K and V are read once, for all heads of the group at a time.  Short calls are bound by latency: lengths, pages, the first block and the
+// and 308.)  Bound by HBM: K and V are read once for 16 heads of a group at a time (fp32: 8).  Short calls are bound by latency: lengths, pages, the first block and the
 // join come one after the other, 6.5 us of a call, and a block takes a wave 1.35 us (fp32 1.8) however little the others read.
 #include "device_utils.h"
 #include "full_cache.h"
@@ -250,24 +250,30 @@ struct Part {
   __device__ __forceinline__ bool whole() const { return block0 == 0 && block1 == n; }
 };
 
+// The group's heads that a workgroup handles; the first ones' workgroups see to what there is once per row.
+struct Heads {
+  int first, n;
+  __device__ __forceinline__ explicit Heads(const CacheAttnParams& p) : first(blockIdx.y * p.heads), n(min(p.heads, p.G - first)) {}
+};
+
 // A row that a wave has for itself.
 template <int D>
-__device__ __forceinline__ void write_row(const CacheAttnParams& p, int row, int lane, const float* acc, const float2* ml) {
-  const int64_t head0 = (int64_t)row * p.G + p.g0;
-  for (int i = lane; i < p.gb * (D / 4); i += 64) {
+__device__ __forceinline__ void write_row(const CacheAttnParams& p, Heads heads, int row, int lane, const float* acc, const float2* ml) {
+  const int64_t head0 = (int64_t)row * p.G + heads.first;
+  for (int i = lane; i < heads.n * (D / 4); i += 64) {
     const float l = ml[i / (D / 4)].y, f = l == 0.f ? 0.f : 1.f / l;
     const float4 a = reinterpret_cast<const float4*>(acc)[i];
     reinterpret_cast<float4*>(p.out + head0 * D)[i] = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(a.x * f, a.y * f, a.z * f, a.w * f);
   }
-  if (p.lse && lane < p.gb) p.lse[head0 + lane] = ml[lane].y == 0.f ? -INFINITY : fmaf(ml[lane].x, p.join_scale, logf(ml[lane].y));
-  if (p.by_row && lane == 0) p.joins[row].first = -1;
+  if (p.lse && lane < heads.n) p.lse[head0 + lane] = ml[lane].y == 0.f ? -INFINITY : fmaf(ml[lane].x, p.join_scale, logf(ml[lane].y));
+  if (p.by_row && heads.first == 0 && lane == 0) p.joins[row].first = -1;
 }
 
 // The end of a workgroup, behind a barrier: its waves' parts, in order, those of a row merged.  Part 2 w is the first one of wave w, 2 w + 1 its last
 // one; part k has its accumulators at acc + k * stride.
 template <int D, int HEADS>
-__device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Shares& shares, const Part (&left)[2 * NW], const float* acc, int stride,
-                                             const float2 (&ml)[2 * NW][HEADS]) {
+__device__ __forceinline__ void finish_group(const CacheAttnParams& p, Heads heads, const Shares& shares, const Part (&left)[2 * NW], const float* acc,
+                                             int stride, const float2 (&ml)[2 * NW][HEADS]) {
   const int group = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const float cexp = p.join_scale * 1.44269502162933349609375f;
   const Part mine = left[lane & (2 * NW - 1)];  // a part per lane
@@ -278,8 +284,8 @@ __device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Sha
     const int last = __builtin_amdgcn_readlane(mine.block1, 31 - __clz(set));
     todo &= ~set;
     const bool begins = __builtin_amdgcn_readlane(mine.block0, k0) == 0, whole = begins && last == n;
-    const int64_t head0 = (int64_t)row * p.G + p.g0, part0 = part_at(p, group, begins) + p.g0;
-    for (int i = tid; i < p.gb * D; i += NW * 64) {
+    const int64_t head0 = (int64_t)row * p.G + heads.first, part0 = part_at(p, group, begins) + heads.first;
+    for (int i = tid; i < heads.n * D; i += NW * 64) {
       const int h = i / D;
       // all parts' numbers, whether they are the row's or not: what is not is left out by its factor
       float2 v[2 * NW];
@@ -311,7 +317,7 @@ __device__ __forceinline__ void finish_group(const CacheAttnParams& p, const Sha
     }
     // Where a row's parts lie is said by the workgroup that begins it: a record per row (of rows without tokens by clear_empty), or, where there are
     // more rows than workgroups, one per workgroup.
-    if (tid == 0 && begins && (!whole || p.by_row)) {
+    if (tid == 0 && heads.first == 0 && begins && (!whole || p.by_row)) {
       JoinRecord r = {row, -1, 0};
       if (!whole) {
         r.first = group;
@@ -445,8 +451,10 @@ __global__ __launch_bounds__(NW * 64, D == 64 && GPAD > 4 ? 1 : 2) void cache_at
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int tq = lane / CH, cl = lane % CH;  // load role: token of a load, 16-byte chunk
   const int n = lane & 15, j = lane >> 4;    // MFMA role: column, row block / k-group
-  const int number = blockIdx.x * NW + wave, g0 = p.g0, gb = p.gb;
-  if (tid == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
+  const int number = blockIdx.x * NW + wave;
+  const Heads heads(p);
+  const int g0 = heads.first, gb = heads.n;
+  if (tid == 0 && g0 == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
   if (lane < 2) s_left[2 * wave + lane].row = -1;
   const int empty = length_of(p, min((int)blockIdx.x, p.P - 1));
   Ahead<BT> ahead;
@@ -660,11 +668,11 @@ __global__ __launch_bounds__(NW * 64, D == 64 && GPAD > 4 ? 1 : 2) void cache_at
         for (int r = 0; r < 4; ++r) s_acc[(4 * j + r) * D + nd * 16 + n] = acc[nd][r];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (whole) write_row<D>(p, part.row, lane, s_acc, s_ml[k]);
+    if (whole) write_row<D>(p, heads, part.row, lane, s_acc, s_ml[k]);
     reset();
   }
   __syncthreads();
-  finish_group<D, GPAD>(p, shares, s_left, reinterpret_cast<const float*>(&lds[0][0][0]), kSpan * 4, s_ml);
+  finish_group<D, GPAD>(p, heads, shares, s_left, reinterpret_cast<const float*>(&lds[0][0][0]), kSpan * 4, s_ml);
   if (g0 == 0) clear_empty(p, empty);
 }
 
@@ -689,8 +697,10 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int t8 = lane >> 3, sl = lane & 7;   // K role: token of a group, share of a token; head, once the logits are summed
   const int tq = lane / CH, cl = lane % CH;  // V role: token of a load, chunk
-  const int number = blockIdx.x * NW + wave, g0 = p.g0;
-  if (tid == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
+  const int number = blockIdx.x * NW + wave;
+  const Heads heads(p);
+  const int g0 = heads.first;
+  if (tid == 0 && g0 == 0 && !p.by_row) p.joins[blockIdx.x].first = -1;
   if (lane < 2) s_left[2 * wave + lane].row = -1;
   const int empty = length_of(p, min((int)blockIdx.x, p.P - 1));
   Ahead<BT> ahead;
@@ -717,7 +727,7 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
   auto load_q = [&](int prob, int c) {
     const float* q = (const float*)p.q + (((int64_t)prob * p.Hkv + c) * p.G + g0) * D;
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) qv[i] = q[i * 64 + lane];
+    for (int i = 0; i < NQ; ++i) qv[i] = i * 64 + lane < heads.n * D ? q[i * 64 + lane] : 0.f;
   };
   auto keep_q = [&] {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -859,45 +869,46 @@ __global__ __launch_bounds__(256, GB <= 4 ? 2 : 1) void cache_attn_f32_kernel(Ca
     l = swap32_sum_f64(l);
     if (lane < GB) s_ml[k][lane] = make_float2(m, (float)l);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (whole) write_row<D>(p, part.row, lane, s_acc[k], s_ml[k]);
+    if (whole) write_row<D>(p, heads, part.row, lane, s_acc[k], s_ml[k]);
     reset();
     if (ahead.valid) keep_q();
   }
   __syncthreads();
-  finish_group<D, GB>(p, shares, s_left, &s_acc[0][0], GB * D, s_ml);
+  finish_group<D, GB>(p, heads, shares, s_left, &s_acc[0][0], GB * D, s_ml);
   if (g0 == 0) clear_empty(p, empty);
 }
 
 template <int D, int GB = 1>
-void launch_f32(const CacheAttnParams& p, hipStream_t s) {
+void launch_f32(const CacheAttnParams& p, dim3 grid, hipStream_t s) {
   if constexpr (GB < 8) {
-    if (p.gb > GB) return launch_f32<D, GB + 1>(p, s);
+    if (p.heads > GB) return launch_f32<D, GB + 1>(p, grid, s);
   }
-  hipLaunchKernelGGL((cache_attn_f32_kernel<D, GB>), dim3((unsigned)((p.n_waves + NW - 1) / NW)), dim3(NW * 64), 0, s, p);
+  hipLaunchKernelGGL((cache_attn_f32_kernel<D, GB>), grid, dim3(NW * 64), 0, s, p);
 }
 
 template <int D>
-void launch_bf16(const CacheAttnParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)((p.n_waves + NW - 1) / NW));
-  if (p.gb <= 4) hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 4>), grid, dim3(256), 0, s, p);
-  else if (p.gb <= 8) hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 8>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 16>), grid, dim3(256), 0, s, p);
+void launch_bf16(const CacheAttnParams& p, dim3 grid, hipStream_t s) {
+  if (p.heads <= 4) hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 4>), grid, dim3(NW * 64), 0, s, p);
+  else if (p.heads <= 8) hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 8>), grid, dim3(NW * 64), 0, s, p);
+  else hipLaunchKernelGGL((cache_attn_bf16_kernel<D, 16>), grid, dim3(NW * 64), 0, s, p);
 }
 
 }  // namespace
 
-hipError_t launch_cache_attn(const CacheAttnParams& p, bool join, hipStream_t s) {
-  CacheAttnParams q = p;
-  const int per = p.dtype == DT_BF16 ? 16 : 8;  // heads a launch handles
-  for (q.g0 = 0; q.g0 < p.G; q.g0 += per) {
-    q.gb = p.G - q.g0 < per ? p.G - q.g0 : per;
-    if (p.dtype == DT_BF16) p.D == 128 ? launch_bf16<128>(q, s) : launch_bf16<64>(q, s);
-    else p.D == 128 ? launch_f32<128>(q, s) : launch_f32<64>(q, s);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+hipError_t launch_cache_attn(const CacheAttnParams& p0, bool join, hipStream_t s) {
+  // Groups of more heads than a workgroup takes: evenly over several, in one launch.  (us, launches one after the other and one launch: fp32, 16 heads, 300 tokens 33.1
+  // 17.1, 524301 tokens x 8 rows 1774 1520; bf16, 32 heads, 32001 tokens 64.2 52.5, 524301 649 641: K and V are read again all the same.)
+  CacheAttnParams p = p0;
+  const int most = p.dtype == DT_BF16 ? 16 : 8, n = (p.G + most - 1) / most;
+  p.heads = (p.G + n - 1) / n;
+  const unsigned groups = (unsigned)((p.n_waves + NW - 1) / NW);
+  const dim3 all(groups, (unsigned)((p.G + p.heads - 1) / p.heads));
+  if (p.dtype == DT_BF16) p.D == 128 ? launch_bf16<128>(p, all, s) : launch_bf16<64>(p, all, s);
+  else p.D == 128 ? launch_f32<128>(p, all, s) : launch_f32<64>(p, all, s);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   if (!join) return hipSuccess;
-  const dim3 grid((unsigned)(p.by_row ? p.P * p.Hkv : (p.n_waves + NW - 1) / NW), (unsigned)p.G);
+  const dim3 grid((unsigned)(p.by_row ? p.P * p.Hkv : groups), (unsigned)p.G);
   if (p.D == 128) hipLaunchKernelGGL(join_kernel<128>, grid, dim3(256), 0, s, p);
   else hipLaunchKernelGGL(join_kernel<64>, grid, dim3(256), 0, s, p);
   return hipGetLastError();

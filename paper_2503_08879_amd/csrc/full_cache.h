@@ -64,7 +64,7 @@ struct CacheAttnParams {
   int S, W, max_len;
   bool by_row;  // a join record per row, else one per workgroup
   int n_waves;
-  int g0, gb;    // the group's heads that a launch handles
+  int heads;     // of a group, a workgroup's at most
   float scale;       // 1 / sqrt(head_dim)
   float join_scale;  // the parts' maxima times this are logits: scale where they are products (bf16), 1 where they are logits (fp32)
   float* part_acc;    // [kAttnGroups][2][G][D]
