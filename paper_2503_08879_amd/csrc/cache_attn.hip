@@ -897,9 +897,13 @@ void launch_bf16(const CacheAttnParams& p, dim3 grid, hipStream_t s) {
 
 hipError_t launch_cache_attn(const CacheAttnParams& p0, bool join, hipStream_t s) {
   // Groups of more heads than a workgroup takes: evenly over several, in one launch.  (us, launches one after the other and one launch: fp32, 16 heads, 300 tokens 33.1
-  // 17.1, 524301 tokens x 8 rows 1774 1520; bf16, 32 heads, 32001 tokens 64.2 52.5, 524301 649 641: K and V are read again all the same.)
+  // 17.1, 524301 tokens x 8 rows 1774 1520; bf16, 32 heads, 32001 tokens 64.2 52.5, 524301 649 641: K and V are read again all the same.)  So are fewer heads
+  // where the rows, at their longest, leave waves without work: the fewer heads, the sooner a block is done, and K and V are read again from the caches.  (us, a workgroup and
+  // several, two rows: fp32, 64 dims, 8 heads, 261 tokens 16.9 9.4, 600 14.4 10.6, 8000 13.9 12.4, 2 heads 10.0 9.3, 10.6 10.4, 10.2 11.0; bf16, 128 dims, 16 heads, 261 13.3 11.1,
+  // 600 15.2 12.3, 4000 13.5 12.4, 7 heads 11.5 11.0, 13.0 12.1, 12.2 12.4.)
   CacheAttnParams p = p0;
-  const int most = p.dtype == DT_BF16 ? 16 : 8, n = (p.G + most - 1) / most;
+  const int most = p.dtype == DT_BF16 ? 16 : 8, least = p.dtype == DT_BF16 ? 4 : 1;
+  const int n = max((p.G + most - 1) / most, min((p.G + least - 1) / least, kAttnWaves / p.n_waves));
   p.heads = (p.G + n - 1) / n;
   const unsigned groups = (unsigned)((p.n_waves + NW - 1) / NW);
   const dim3 all(groups, (unsigned)((p.G + p.heads - 1) / p.heads));

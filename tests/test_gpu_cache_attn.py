@@ -118,6 +118,14 @@ def test_heads_per_group(dtype, d, G):
 
 
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 2, 3, 4, 5, 6, 7, 8, 9, 11, 16, 17, 24, 33, 64])
+def test_heads_per_group_beside_longer_rows(dtype, d, G):
+    """Rows of which one may be long keep all heads that a workgroup can take with one workgroup; short ones' heads are spread."""
+    case([600, 3, 0, 1300], 2 * G, 2, d, dtype, cap=8200, seed=G)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 @pytest.mark.parametrize("n", [1, 2, 16, 128, 129, 256, 257, 384, 640, 5000, 70001])
 def test_one_sequence(dtype, n):
     """Rows from one token to many steps, alone and with a capacity beyond them."""
