@@ -84,22 +84,24 @@ struct ProblemSearch {
   }
 };
 
-template <int DT, int MODE, int D>
+// T tokens per wave, next to each other, in equal shares of its lanes.
+template <int DT, int MODE, int D, int T>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   constexpr int EB = DT == DT_BF16 ? 2 : 4, NP = Part<DT>::N;
-  constexpr int LPT = D / (2 * NP), HS = 64 / LPT;  // lanes a head's row is shared by; heads a wave takes at a time
+  constexpr int LPT = D / (2 * NP), HS = 64 / T / LPT;  // lanes a head's row is shared by; heads of a token at a time
   constexpr int U = 4;                              // rounds of heads in flight
-  __shared__ float2 turn[4][64];
+  __shared__ float2 turn[4][T][64];
   __shared__ uint4 copy[MODE == APART ? 4 : 1][MODE == APART ? 128 : 1];  // APART: a wave's rows
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t t64 = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t t64 = ((int64_t)blockIdx.x * 4 + wave) * T;
   if (t64 >= p.n_tokens) return;
-  const int t = (int)t64;
+  const int t0 = (int)t64, k = lane / (64 / T), t = min(t0 + k, (int)p.n_tokens - 1);  // the wave's first token, which of them this lane's is
+  bool real = t0 + k < p.n_tokens;
 
   // The token's rows are asked for early: what is done with them waits for its position, which is up to five memory round trips away (the problem's number,
   // its offsets, its length, the page).
-  const int slot = lane / LPT, cl = lane % LPT;
+  const int slot = lane % (64 / T) / LPT, cl = lane % LPT;
   const bool rotates = cl * NP < p.r;
   const int e0 = cl * NP, e1 = D / 2 + e0, half = p.r / 2;  // first elements of this lane's two parts of a row
   const int at0 = e0 * EB, at1 = e1 * EB;
@@ -124,7 +126,15 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   };
   ProblemSearch search = {1, 0};
   if (p.offsets) search.ask(p.offsets, 0, p.P, lane);
-  const double freq = lane < p.r / 2 ? p.freq[lane] : 0.0;
+  // angle i * 64 + lane is pair `pair[i]` of token `of[i]`
+  double freq[T];
+  int of[T], pair[T];
+#pragma unroll
+  for (int i = 0; i < T; ++i) {
+    of[i] = T == 1 || half == 0 ? 0 : (i * 64 + lane) / half;
+    pair[i] = i * 64 + lane - of[i] * half;
+    freq[i] = i * 64 + lane < T * half ? p.freq[pair[i]] : 0.0;
+  }
   load(h0);
 
   // the token's problem and place
@@ -134,14 +144,30 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     int count = 1, i = 0;
     prob = t;
     if (p.offsets) {
-      prob = search.find(p.offsets, p.P, t, lane);
-      if (prob >= p.P || t < p.offsets[0]) return;  // nobody's row
+      const int prob0 = search.find(p.offsets, p.P, t0, lane);
+      prob = prob0;
+      if (T > 1) {  // the others' problems are that one or, rarely, later ones
+        const int at = prob0 + 1 + lane, end = p.offsets[min(at, p.P)];
+#pragma unroll
+        for (int j = 1; j < T; ++j) {
+          const int ended = __popcll(__ballot(at <= p.P && end <= t0 + j));
+          int other = prob0 + ended;
+          if (ended == 64) {  // many problems without tokens between them
+            search.ask(p.offsets, 0, p.P, lane);
+            other = search.find(p.offsets, p.P, t0 + j, lane);
+          }
+          prob = k == j ? other : prob;
+        }
+      }
+      real = real && prob < p.P && t >= p.offsets[0];  // else it is nobody's row
+      if (T == 1 && !real) return;
+      prob = min(prob, p.P - 1);
       const int begin = p.offsets[prob];
       count = p.offsets[prob + 1] - begin;
       i = t - begin;
     }
     place = p.lens[prob] - count + i;
-    stored = place >= 0 && place < p.capacity;
+    stored = real && place >= 0 && place < p.capacity;
   }
   int64_t block = prob;
   if (stored && p.cache.table) {
@@ -150,13 +176,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   }
   const int64_t in_block = place & (int)((1u << p.cache.shift) - 1u);
 
-  // cosines and sines of the token's pairs
-  if (lane < p.r / 2) {
+  // cosines and sines of the tokens' pairs
+  if (p.r > 0) {
     const int pos = p.positions ? p.positions[t] : place;
-    const double turns = (double)pos * (freq * 0.15915494309189533577);  // 1 / (2 pi)
-    float s, c;
-    sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-    turn[wave][lane] = make_float2(p.amplitude * c, p.amplitude * p.sign * s);
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+      if (i * 64 >= T * half) break;
+      const int pos_i = T == 1 ? pos : __shfl(pos, of[i] * (64 / T));
+      if (i * 64 + lane >= T * half) continue;
+      const double turns = (double)pos_i * (freq[i] * 0.15915494309189533577);  // 1 / (2 pi)
+      float s, c;
+      sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+      turn[wave][of[i]][pair[i]] = make_float2(p.amplitude * c, p.amplitude * p.sign * s);
+    }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   // HALVES: of the pairs that both parts share; PAIRS: of the first part's, then the second's; APART: of the elements, sines with their signs
@@ -165,18 +197,18 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   if (rotates) {
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int e = MODE == HALVES ? 0 : i < NC / 2 ? e0 : e1, k = i % (NC / 2);
-      const int j = MODE == HALVES ? e0 + i : MODE == PAIRS ? e / 2 + k : e + k < half ? e + k : e + k - half;
-      const float2 v = turn[wave][min(j, 63)];  // (behind the last pair: not used)
+      const int e = MODE == HALVES ? 0 : (i < NC / 2 ? e0 : e1) + (MODE == APART ? i % (NC / 2) : 0);
+      const int j = MODE == HALVES ? e0 + i : MODE == PAIRS ? e / 2 + i % (NC / 2) : e < half ? e : e - half;
+      const float2 v = turn[wave][k][min(j, 63)];  // (behind the last pair: not used)
       cs[i] = v.x;
-      sn[i] = MODE == APART && e + k < half ? -v.y : v.y;
+      sn[i] = MODE == APART && e < half ? -v.y : v.y;
     }
   }
 
   char* qd = p.q_out.base + (int64_t)t * p.q_out.token;
   char* kd = p.cache.K + block * p.cache.ks_block + in_block * p.cache.ks_token;
   char* vd = p.cache.V + block * p.cache.vs_block + in_block * p.cache.vs_token;
-  const int h1 = min(stored ? all : p.Hq, h0 + per);
+  const int h1 = real ? min(stored ? all : p.Hq, h0 + per) : 0, last = T == 1 ? h1 : min(all, h0 + per);
   for (int hb = h0;;) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -204,7 +236,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
           a[u].set_first(y[0], p.r - e0);
           b[u].set_first(y[1], p.r - e1);
         } else {
-          char* row = (char*)copy[wave] + slot * (D * EB);
+          char* row = (char*)copy[wave] + lane / LPT * (D * EB);
           __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
           *(uint4*)(row + at0) = a[u].u;
           *(uint4*)(row + at1) = b[u].u;
@@ -226,7 +258,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
       b[u].store(dst + at1);
     }
     hb += U * HS;
-    if (hb >= h1) break;
+    if (hb >= last) break;
     load(hb);
   }
 }
@@ -237,8 +269,17 @@ hipError_t launch_rotary_m(const RotaryParams& p, hipStream_t s) {
   // few tokens: their heads over several waves (latency)
   const int64_t want = (1024 + p.n_tokens - 1) / p.n_tokens;
   const dim3 grid((unsigned)((p.n_tokens + 3) / 4), (unsigned)(want < rounds ? want : rounds));
-  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64>), grid, dim3(256), 0, s, p);
+  // Tokens that fill at most half of a wave's lanes, and enough of them for all SIMDs: four per wave, so that the way to their places, five memory round trips, is gone
+  // once for all.  (us, one and four tokens per wave, bf16: 160000 tokens of 4 + 2 heads, 64 dims 100 72, with 20 of them rotated 166 92; 16000 tokens' queries, 4 heads of 64 dims 8.5
+  // 5.6; 32767, 4 heads of 128 dims 16.0 13.8; more than half: 8 heads of 128 dims 21.6 22.2, 160000 tokens of 16 + 1 heads of 128 dims 243 300.)
+  if (heads <= HS / 2 && p.n_tokens >= 4096) {
+    const dim3 fewer((unsigned)((p.n_tokens + 15) / 16));
+    if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128, 4>), fewer, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, 4>), fewer, dim3(256), 0, s, p);
+    return hipGetLastError();
+  }
+  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128, 1>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, 1>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -123,6 +123,17 @@ def test_many_problems_most_of_them_without_new_tokens(P):
     case(P, 2, 1, 64, 20, new, [a + p % 10 for p, a in enumerate(new)], pad=3)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("r,layout,inplace", [(64, 0, False), (20, 0, True), (20, 1, False), (64, 1, True), (0, 0, False)])
+def test_many_tokens_of_few_heads(dtype, r, layout, inplace):
+    """Problems of one token, of none (a hundred in a row), of many; rows behind the last one; one token each of as many problems."""
+    new = [1] * 101 + [0] * 150 + [2, 0, 3, 1] * 70 + [0] * 66 + [613, 0, 0, 1500, 7, 1490] + [0] * 5
+    assert sum(new) >= 4096
+    lens = [a + p % 13 for p, a in enumerate(new)]
+    case(len(new), 2, 1, 64, 1520, new, lens, dtype, r, layout, pad=5, inplace=inplace, amplitude=0.75)
+    case(4099, 2, 1, 64, 9, [1] * 4099, [p % 11 for p in range(4099)], dtype, r, layout, dense=True, order="tokens", single=True)
+
+
 def test_rows_in_front_of_the_first_problem_are_left_out():
     import torch
 

@@ -50,6 +50,15 @@ def test_shapes_layouts_and_parts(dtype, layout, n, H, d, r):
     check(x, pos, back, freq, layout, 0.5, True)
 
 
+@pytest.mark.parametrize("dtype,H,d", [("bfloat16", 4, 128), ("bfloat16", 7, 64), ("float32", 2, 128), ("float32", 4, 64)])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("n,r", [(4096, 64), (4099, 20), (5001, 2), (4098, 48)])
+def test_many_tokens_of_few_heads(dtype, H, d, layout, n, r):
+    test_shapes_layouts_and_parts(dtype, layout, n, H, d, r)
+    if r == 64:
+        test_shapes_layouts_and_parts(dtype, layout, n, H, d, d)
+
+
 @pytest.mark.parametrize("r", [128, 20])
 def test_far_positions_and_the_ends_of_int32(r):
     """Angles of 2^31 turns' order lose nothing: they are reduced in fp64 (an error of 2^31 * 2^-53 radians)."""
