@@ -278,8 +278,12 @@ hipError_t launch_rotary_m(const RotaryParams& p, hipStream_t s) {
     else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, 4>), fewer, dim3(256), 0, s, p);
     return hipGetLastError();
   }
-  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128, 1>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, 1>), grid, dim3(256), 0, s, p);
+  // Tokens of 8 KB and more keep a wave's registers full of loads, and four workgroups per CU read and write faster than six or seven: LDS that nobody uses keeps others away.  (us,
+  // bf16, 128 dims, seven, four and three workgroups: 131072 tokens of 32 + 8 heads 617 567 615, 16384 79.1 74.2 83.1, fp32 1259 1168 1235; smaller tokens, 32767 of 28 heads 85.6 86.5
+  // 97.4, with 64 dims 45.2 48.7 56.1; fewer, whose last workgroups then run alone, 6532 of 32 + 8 heads 26 31.)
+  const unsigned unused = p.n_tokens >= 16384 && p.D * heads * (16 / Part<DT>::N) >= 8192 ? 36000 - (MODE == APART ? 8192 : 0) : 0;
+  if (p.D == 128) hipLaunchKernelGGL((rotary_kernel<DT, MODE, 128, 1>), grid, dim3(256), unused, s, p);
+  else hipLaunchKernelGGL((rotary_kernel<DT, MODE, 64, 1>), grid, dim3(256), unused, s, p);
   return hipGetLastError();
 }
 
