@@ -262,7 +262,7 @@ sagekv_status sagekv_decode_step_paged(const sagekv_decode_desc* desc, const sag
  *   q_sink = the query rotated at position n-1 = S+k+W-1 (a sink token's absolute position IS its
  *            window position, so only the query's position differs),
  * and the sink tokens [0, n_sink) are scored with q_sink, every other token with q.  The rotation
- * itself belongs to the model around the cache and is not done here.  Everything else is as in
+ * itself is not done here (sagekvc_rotary of sagekv_cache.h does it).  Everything else is as in
  * sagekv_decode_attn / sagekv_decode_step; q_sink [n_problems, Hq, head_dim] must not be null. */
 sagekv_status sagekv_decode_attn_window(const sagekv_decode_desc* desc, const void* q, const void* q_sink,
                                         const void* Kc, const void* Vc, int32_t len, float* out, void* workspace,

@@ -108,7 +108,7 @@ sagekv_status check_cache(const sagekvc_desc* d, const sagekv_paged_kv* pg, cons
   }
   if (!strides_ok(k, 3, d->dtype) || !strides_ok(v, 3, d->dtype) || !aligned(K, 16) || !aligned(V, 16)) return SAGEKV_ERR_UNSUPPORTED;
   if (k[2] < d->head_dim || v[2] < d->head_dim) return SAGEKV_ERR_UNSUPPORTED;  // as in the eviction pass
-  const int64_t most = (1 << 24) / element_bytes(d->dtype);  // 24 bits: see token_at in cache_attn.hip
+  const int64_t most = (1 << 24) / element_bytes(d->dtype);  // 24 bits: see load_token in cache_attn.hip
   if (k[2] >= most || v[2] >= most) return SAGEKV_ERR_UNSUPPORTED;
   if (written && (rows_overlap(k, n, 3, d->head_dim) || rows_overlap(v, n, 3, d->head_dim))) return SAGEKV_ERR_INVALID_ARG;
   const int eb = element_bytes(d->dtype);

@@ -99,10 +99,6 @@ def _ints(t, n, device):
     return t.data_ptr()
 
 
-def _ref(struct):
-    return None if struct is None else ctypes.byref(struct)
-
-
 def _place(struct):
     """Address of a descriptor (ctypes.byref makes an object per call)."""
     return None if struct is None else ctypes.addressof(struct)
