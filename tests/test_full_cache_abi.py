@@ -173,7 +173,7 @@ CACHE_REFUSALS = [
 ])
 def test_write_refusals(code, paged, change):
     desc, pages, tokens, rot, a = cache_args(paged, **change)
-    got = fc._fn("sagekvc_write")(byref(desc), fc._ref(pages), byref(tokens), byref(rot), a["q"], a["k"], a["v"], a["offsets"], a["lens"], a["pos"],
+    got = fc._fn("sagekvc_write")(byref(desc), fc._place(pages), byref(tokens), byref(rot), a["q"], a["k"], a["v"], a["offsets"], a["lens"], a["pos"],
                                   a["q_out"], a["K"], a["V"], None)
     assert got == code
 
@@ -200,7 +200,7 @@ def test_attn_refusals(code, paged, change):
     size = sk.sagekvc_attn_workspace_bytes(cache_args(paged)[0])
     assert size > 0
     desc, pages, _, _, a = cache_args(paged, **{k: v for k, v in change.items() if k not in own})
-    got = fc._fn("sagekvc_attn")(byref(desc), fc._ref(pages), a["q"], a["K"], a["V"], a["lens"], own["max_len"], own["S"], own["W"], own["out"], own["lse"],
+    got = fc._fn("sagekvc_attn")(byref(desc), fc._place(pages), a["q"], a["K"], a["V"], a["lens"], own["max_len"], own["S"], own["W"], own["out"], own["lse"],
                                  own["ws"], size - own["short"], None)
     assert got == code
 
